@@ -45,6 +45,7 @@
 
 #include "quest_internal.cuh"
 #include "quest_operand.cuh"
+#include "quest_tcgen05.cuh"
 
 namespace quest {
 namespace {
@@ -54,9 +55,6 @@ constexpr int BK = 128;          // bytes (= int8 elements) of K per pipeline st
 constexpr int UMMA_K = 32;       // K per tcgen05.mma kind::i8
 constexpr int EPI_WARPS = 8;     // two per TMEM lane quarter, each taking half of the tile's columns
 constexpr int NUM_THREADS = 64 + 32 * EPI_WARPS;
-constexpr long long WAIT_LIMIT_CYCLES = 4000000000LL;   // ~2 s at 2 GHz
-
-enum { ST_OK = 0, ST_PRODUCER = 1, ST_MMA = 2, ST_EPILOGUE = 3 };
 
 struct GemmParams {
     int M, N, K;           // K: bytes of the contraction per operand row (int8: elements; bf16: 2 x elements)
@@ -84,76 +82,6 @@ struct GemmParams {
     float iht_scale = 0.0f;
 };
 
-__device__ __forceinline__ uint32_t smem_u32(const void *p) {
-    return (uint32_t)__cvta_generic_to_shared(p);
-}
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-// Bounded wait.  Returns false if the CTA is aborting or the limit expired (then it records
-// `code` in the device status word and raises the CTA-wide abort flag).
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int *abort_flag,
-                                            int *status, int code, long long limit_cycles) {
-    const long long t0 = clock64();
-    for (uint32_t it = 0; it < 0x7fffffffu; ++it) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if ((it & 15u) == 15u) {
-            if (*abort_flag) return false;
-            if (clock64() - t0 > limit_cycles) break;
-        }
-    }
-    *abort_flag = 1;
-    atomicExch(status, code);
-    return false;
-}
-
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status, int code,
-                                          long long limit_cycles = WAIT_LIMIT_CYCLES) {
-    if (mbar_try_wait(bar, parity)) return true;
-    return mbar_wait_slow(bar, parity, abort_flag, status, code, limit_cycles);
-}
-
-// One thread of a converged warp.  The tensor-core and copy instructions take their operands from uniform registers;
-// behind elect.sync the compiler knows that a single thread executes them, behind a test of the lane index it does not:
-// then a k-block costs the issuing threads about 620 cycles whatever the tile, more than the 524 the tensor cores need
-// for a 256 x 256 tile.  With it (and the inlined first try of the waits) the main loop runs at 516 cycles per k-block:
-// 4096 x 2048 x 2048 17.4 -> 15.8 us, 8192 x 5504 x 2048 71.9 -> 65.6 us (with zeros for operands, which draw less power,
-// 16.1 -> 14.0 and 65.5 -> 55.9 us).
-__device__ __forceinline__ bool elect_one() {
-    uint32_t is;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "elect.sync _|p, 0xffffffff;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(is));
-    return is != 0;
-}
-
-// Shared-memory matrix descriptor: K-major operand, 128-byte swizzle, rows of 128 bytes,
-// 8-row groups 1024 bytes apart.
-__device__ __forceinline__ uint64_t make_smem_desc(uint32_t smem_addr) {
-    uint64_t d = 0;
-    d |= (uint64_t)((smem_addr & 0x3FFFF) >> 4);          // start address, bits [0,14)
-    d |= (uint64_t)1 << 16;                                // leading byte offset (unused with swizzle), bits [16,30)
-    d |= (uint64_t)(1024 >> 4) << 32;                      // stride byte offset, bits [32,46)
-    d |= (uint64_t)1 << 46;                                // descriptor version (sm_100), bits [46,48)
-    d |= (uint64_t)2 << 61;                                // layout: SWIZZLE_128B, bits [61,64)
-    return d;
-}
 // The same for an MN-major 16-bit operand as TMA lays it out: rows of 128 bytes hold 64 consecutive
 // elements of the M (or N) dimension for one k; eight consecutive k form a 1024-byte swizzle atom;
 // the next eight k follow 1024 bytes later (stride byte offset), the next 64 elements of M / N
@@ -195,39 +123,6 @@ __device__ __forceinline__ void tmem_st4(uint32_t taddr, uint32_t v) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(v), "r"(v), "r"(v), "r"(v)
                  : "memory");
 }
-__device__ __forceinline__ uint32_t cluster_ctarank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-// shared::cluster address of the same shared-memory offset in CTA `rank` of this cluster
-__device__ __forceinline__ uint32_t mapa_shared(uint32_t addr, uint32_t rank) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// The two halves of the cluster barrier on their own: a warp arrives as soon as it has nothing left to publish to
-// the peer CTA and waits only where it needs the peer, so the barrier's latency overlaps the work between.
-__device__ __forceinline__ void cluster_arrive() {
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_wait() {
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-// cta_group::2 forms: the load may signal an mbarrier of the peer CTA; the MMA spans both CTAs of
-// the pair; the commit arrives on the same barrier offset in every CTA named by the mask.
-__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *tm, int c0, int c1, uint32_t cluster_bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(cluster_bar), "r"(c0), "r"(c1)
-        : "memory");
-}
 __device__ __forceinline__ void umma_i8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
                                              uint32_t accumulate) {
     asm volatile(
@@ -246,47 +141,7 @@ __device__ __forceinline__ void umma_bf16_pair(uint32_t d_tmem, uint64_t a_desc,
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"((uint16_t)3)
-                 : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
 constexpr int MAX_STAGES = 6;
-
-// Tile order: m fastest inside bands of RASTER_M row tiles, bands one after another.  Concurrent CTAs
-// then share one or two column tiles of B while the rows of A a band touches (RASTER_M x TILE_M x K
-// bytes) stay in L2 for all of the band's column tiles; with a single band (up to RASTER_M row tiles)
-// this is plain column-major order.
-constexpr int RASTER_M = 16;
-__device__ __forceinline__ void tile_coords(int tile, int num_m, int num_n, int &tm, int &tn) {
-    const int band_tiles = RASTER_M * num_n;
-    const int band = tile / band_tiles;
-    const int t = tile - band * band_tiles;
-    const int rows_here = min(RASTER_M, num_m - band * RASTER_M);
-    tn = t / rows_here;
-    tm = band * RASTER_M + (t - tn * rows_here);
-}
-
-// 32 columns of this warp's 32 TMEM lanes, issued without waiting: the registers are valid only
-// after tmem_wait_ld() and pin() (an empty volatile asm that makes every later use depend on a
-// statement ordered after the wait).
-__device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t *r) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr)
-        : "memory");
-}
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void pin(uint32_t &v) { asm volatile("" : "+r"(v)::"memory"); }
 
 // Shared memory of a CTA, from a 1024-byte-aligned base: output staging, barriers, the column-scale tiles (and the
 // column corrections of 8-bit codes, CBT), then the operand ring.  The ring takes as many stages as the launch's
@@ -1109,89 +964,6 @@ __global__ void bounded_wait_probe_kernel(long long limit_cycles, int *status, i
     }
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn get_encode_fn() {
-    static EncodeTiledFn fn = nullptr;
-    if (!fn) {
-        void *ptr = nullptr;
-        cudaDriverEntryPointQueryResult qres;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &qres) != cudaSuccess ||
-            qres != cudaDriverEntryPointSuccess)
-            return nullptr;
-        fn = reinterpret_cast<EncodeTiledFn>(ptr);
-    }
-    return fn;
-}
-
-// Encoding a tensor map is a driver call of a microsecond or two, and a layer that is called again and again
-// passes the same pointers and shapes every time.  Each host thread keeps the last few descriptors it built, keyed
-// by everything that goes into them (a descriptor is a pure function of its key, so a hit is always valid).
-struct MapKey {
-    const void *base;
-    int64_t d0, d1, pitch;
-    int box0, box1, swizzle, promo;
-    bool operator==(const MapKey &o) const {
-        return base == o.base && d0 == o.d0 && d1 == o.d1 && pitch == o.pitch && box0 == o.box0 && box1 == o.box1 &&
-               swizzle == o.swizzle && promo == o.promo;
-    }
-};
-struct MapCache {
-    static constexpr int N = 16;
-    MapKey key[N];
-    CUtensorMap map[N];
-    int used = 0, next = 0;
-    const CUtensorMap *find(const MapKey &k) const {
-        for (int i = 0; i < used; ++i)
-            if (key[i] == k) return &map[i];
-        return nullptr;
-    }
-    void put(const MapKey &k, const CUtensorMap &m) {
-        key[next] = k;
-        map[next] = m;
-        next = (next + 1) % N;
-        if (used < N) ++used;
-    }
-};
-static thread_local MapCache t_map_cache;
-
-// int8 matrix [rows x K], K contiguous; box = 128 bytes of K x box_rows rows, 128-byte swizzle.
-int make_operand_map(CUtensorMap *tm, const int8_t *base, int64_t rows, int64_t K, int box_rows) {
-    const MapKey mk = {base, K, rows, K, BK, box_rows, 1, 1};
-    if (const CUtensorMap *hit = t_map_cache.find(mk)) { *tm = *hit; return QUEST_OK; }
-    EncodeTiledFn fn = get_encode_fn();
-    if (!fn) return cuda_fail_msg("cuTensorMapEncodeTiled entry point not available");
-    cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)K};
-    cuuint32_t box[2] = {(cuuint32_t)BK, (cuuint32_t)box_rows};
-    cuuint32_t estr[2] = {1, 1};
-    CUresult r = fn(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t *>(base), dims, strides, box, estr,
-                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) return cuda_fail_msg("cuTensorMapEncodeTiled failed");
-    t_map_cache.put(mk, *tm);
-    return QUEST_OK;
-}
-
-// y viewed as bytes: [rows x row_bytes], row pitch pitch_bytes; box = 128 bytes x 32 rows, 128-byte swizzle.
-int make_output_map(CUtensorMap *tm, void *base, int64_t rows, int64_t row_bytes, int64_t pitch_bytes) {
-    const MapKey mk = {base, row_bytes, rows, pitch_bytes, 128, 32, 1, 0};
-    if (const CUtensorMap *hit = t_map_cache.find(mk)) { *tm = *hit; return QUEST_OK; }
-    EncodeTiledFn fn = get_encode_fn();
-    if (!fn) return cuda_fail_msg("cuTensorMapEncodeTiled entry point not available");
-    cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)pitch_bytes};
-    cuuint32_t box[2] = {128, 32};
-    cuuint32_t estr[2] = {1, 1};
-    CUresult r = fn(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) return cuda_fail_msg("cuTensorMapEncodeTiled failed for the output");
-    t_map_cache.put(mk, *tm);
-    return QUEST_OK;
-}
-
 // 128-column tiles or 256-column tiles for an M x N product with rows of `row_bytes` operand bytes.  Rounds of the CTA
 // pairs, narrow : wide, decide, and for short rows what the epilogue costs.  Time with narrow tiles over time with wide
 // ones, random operands, medians over shapes of each kind:
@@ -1242,6 +1014,52 @@ int launch_forward(bool narrow, bool yt, const CUtensorMap &tmA, const CUtensorM
 }
 
 }  // namespace
+
+// Encoding a tensor map is a driver call of a microsecond or two, and a layer that is called again and again
+// passes the same pointers and shapes every time.  Each host thread keeps the last few descriptors it built, keyed
+// by everything that goes into them (a descriptor is a pure function of its key, so a hit is always valid).
+int make_map(CUtensorMap *tm, const MapSpec &spec) {
+    typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                      const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                      CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    constexpr int kept = 16;
+    struct Cache {
+        MapSpec key[kept];
+        CUtensorMap map[kept];
+        int used = 0, next = 0;
+    };
+    static thread_local Cache cache;
+    for (int i = 0; i < cache.used; ++i)
+        if (cache.key[i] == spec) { *tm = cache.map[i]; return QUEST_OK; }
+    static EncodeTiledFn fn = nullptr;
+    if (!fn) {
+        void *ptr = nullptr;
+        cudaDriverEntryPointQueryResult qres;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &qres) != cudaSuccess ||
+            qres != cudaDriverEntryPointSuccess)
+            return cuda_fail_msg("cuTensorMapEncodeTiled entry point not available");
+        fn = reinterpret_cast<EncodeTiledFn>(ptr);
+    }
+    const cuuint64_t dims[2] = {(cuuint64_t)spec.d0, (cuuint64_t)spec.d1}, strides[1] = {(cuuint64_t)spec.pitch};
+    const cuuint32_t box[2] = {(cuuint32_t)spec.box0, (cuuint32_t)spec.box1}, estr[2] = {1, 1};
+    if (fn(tm, spec.type, 2, const_cast<void *>(spec.base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, spec.swizzle,
+           spec.promo, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return cuda_fail_msg("cuTensorMapEncodeTiled failed");
+    cache.key[cache.next] = spec;
+    cache.map[cache.next] = *tm;
+    cache.next = (cache.next + 1) % kept;
+    if (cache.used < kept) ++cache.used;
+    return QUEST_OK;
+}
+
+int make_operand_map(CUtensorMap *tm, const int8_t *base, int64_t rows, int64_t K, int box_rows) {
+    return make_map(tm, {base, K, rows, K, BK, box_rows});
+}
+
+int make_output_map(CUtensorMap *tm, void *base, int64_t rows, int64_t row_bytes, int64_t pitch_bytes) {
+    return make_map(tm, {base, row_bytes, rows, pitch_bytes, 128, 32, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_128B,
+                         CU_TENSOR_MAP_L2_PROMOTION_NONE});
+}
 
 int launch_bounded_wait_probe(long long limit_cycles, int *report, cudaStream_t st) {
     int *status = device_status_word();
