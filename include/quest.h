@@ -56,7 +56,8 @@ typedef enum quest_status {
     QUEST_ERR_DEVICE = 10,        /* current device is not compute capability 10.x */
     QUEST_ERR_CUDA = 11,          /* a CUDA runtime/driver call failed; see quest_last_cuda_error() */
     QUEST_ERR_DEVICE_TIMEOUT = 12,/* a bounded wait inside a kernel expired (see quest_device_status) */
-    QUEST_ERR_STATIC_LIMIT = 13   /* quest_lowbit_gemm_static: problem needs more than QUEST_STATIC_SCRATCH_BYTES */
+    QUEST_ERR_STATIC_LIMIT = 13,  /* quest_lowbit_gemm_static: problem needs more than QUEST_STATIC_SCRATCH_BYTES */
+    QUEST_ERR_EPS = 14            /* eps negative, infinite or NaN */
 } quest_status;
 
 enum { QUEST_F32 = 0, QUEST_BF16 = 1 };
@@ -315,6 +316,103 @@ int quest_linear_fwd_weight_only(const void *x, int x_dtype, int64_t ldx, const 
                                  void *y, int y_dtype, int64_t ldy, void *xh, uint8_t *wq, float *sw, uint8_t *mw,
                                  void *workspace, size_t workspace_bytes, void *stream);
 size_t quest_weight_only_workspace_bytes(int64_t M, int64_t N, int64_t K);
+
+/*
+ * Microscaled (MX) layer -- beside the FP4 grid of Section 4.4, whose rows have one binary32 scale: here 32 consecutive
+ * elements of a row share a power-of-two scale (OCP Microscaling Formats 1.0), which the tensor cores apply by themselves.
+ * Weights are MXFP4 (E2M1 elements); activations MXFP4 or MXFP8 (E4M3).  The paper has no counterpart.
+ *
+ *   had_block 32   v = H_32 x / sqrt(32) on every block: binary32, strides 16, 8, 4, 2, 1, then one product with the binary32
+ *                  number nearest to 1/sqrt(32).  The rotation of both operands cancels in their product.
+ *   had_block 1    v = x
+ *   scale byte s = clamp(floor(log2 max|v|) - emax, -127, 127) + 127, emax = 2 (E2M1) or 8 (E4M3); 0 for a block of
+ *                  zeros; 255 (NaN) for a block that holds an infinity or a NaN, whose codes are 0
+ *   code         = v 2^(127 - s) rounded to the nearest element, ties to even, saturating at +-6 or +-448
+ *
+ * Codes and scales are reproducible bit for bit.  Every product with a block of scale 255 is NaN.
+ *
+ *   codes    bits 4: two to a byte, element 0 in the low nibble (sign << 3 | magnitude index); bits 8: E4M3 bytes.  Dense rows.
+ *   scales   quest_mx_scales_bytes(rows, cols) = ceil(rows/128) ceil(cols/128) 512 bytes: tiles of 128 rows x 4 blocks, those
+ *            of 128 rows one after another; row r, block j of a tile at byte 16 (r mod 32) + 4 (r div 32) + j.  Bytes of
+ *            rows and blocks that only fill a tile up are 0 in what the library writes; in what a caller lays out by itself those
+ *            of blocks may be anything but 255 and those of rows anything.
+ *
+ * quest_quantize_mx: rows of x (dtype, row stride ld_elems, 16-byte aligned rows) -> codes (16-byte aligned) and scales.
+ *   0 <= rows <= 2^24; cols a multiple of 32, 32 <= cols <= 16384.
+ * quest_dequantize_mx: codes and scales -> dense rows of the values (rotated where they were rotated), exact in binary32
+ *   and, down to 2^-133, in bfloat16; values past the largest number of the type, which quantize_mx does not make, are infinities.
+ */
+size_t quest_mx_scales_bytes(int64_t rows, int64_t cols);
+int quest_quantize_mx(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld_elems, int bits, int had_block,
+                      uint8_t *codes, uint8_t *scales, void *stream);
+int quest_dequantize_mx(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, int bits,
+                        void *out, int out_dtype, void *stream);
+
+/*
+ * quest_gemm_mx -- y[m][n] = sum_k x[m][k] w[n][k] over the values of two MX tensors, products exact, sums binary32 in an
+ * order that the hardware chooses.
+ *   xq, sx, bits_x   codes [M x K] and scales of x, 4 or 8 bits; 16-byte aligned
+ *   wq, sw           codes [N x K/2] and scales of w, 4 bits; 16-byte aligned, wq 32-byte aligned beside 8-bit x
+ *   K                a multiple of 32 (128 beside 8-bit x), at most 16384
+ *   y                device out [M x N], y_dtype, row stride ldy_elems
+ *
+ * quest_linear_fwd_mx -- the layer: x (and w unless w_is_cached is 1) quantized as quest_quantize_mx does, then the product.
+ *   xq, sx           device out: codes and scales of x, for a backward pass; both may be NULL for M <= 32, where x is then
+ *                    quantized inside the product and nothing but y is written
+ *   wq, sw           device out, or inputs with w_is_cached = 1 (w may be NULL then)
+ * No workspace.  Errors as for quest_linear_fwd.
+ */
+int quest_gemm_mx(const uint8_t *xq, const uint8_t *sx, int bits_x, const uint8_t *wq, const uint8_t *sw,
+                  int64_t M, int64_t N, int64_t K, void *y, int y_dtype, int64_t ldy_elems, void *stream);
+int quest_linear_fwd_mx(const void *x, int x_dtype, int64_t ldx, const void *w, int w_dtype, int64_t ldw,
+                        int64_t M, int64_t N, int64_t K, int bits_x, int had_block, void *y, int y_dtype, int64_t ldy_elems,
+                        uint8_t *xq, uint8_t *sx, uint8_t *wq, uint8_t *sw, int w_is_cached, void *stream);
+
+/*
+ * quest_linear_bwd_mx -- gradients of that layer, straight through the rounding: with IHT the inverse of the block rotation
+ *     dx = IHT(dy w_q),   dw = IHT(dy^T x_q)
+ * As in quest_linear_bwd the products have bfloat16 operands and binary32 sums; the values of MX tensors are exact in
+ * bfloat16.  dy [M x N] bfloat16, dense, 16-byte aligned; M, N > 0 and multiples of 8; dx [M x K], dw [N x K] dense,
+ * out_dtype, 16-byte aligned, either may be NULL; workspace of at least quest_bwd_mx_workspace_bytes(M, N, K) bytes,
+ * 256-byte aligned.
+ */
+int quest_linear_bwd_mx(const void *dy, int64_t M, int64_t N, int64_t K, int bits_x, int had_block,
+                        const uint8_t *xq, const uint8_t *sx, const uint8_t *wq, const uint8_t *sw,
+                        void *dx, void *dw, int out_dtype, void *workspace, size_t workspace_bytes, void *stream);
+size_t quest_bwd_mx_workspace_bytes(int64_t M, int64_t N, int64_t K);
+
+/*
+ * Root-mean-square norm in front of a layer, with the addition of the residual stream (the Llama-style blocks of the paper's
+ * experiments):
+ *     h    = x + residual, rounded to their type (x itself without a residual)
+ *     rstd = (mean(h^2) + eps)^(-1/2)          one binary32 per row; sums in binary32
+ *     y    = (h rstd) weight                   rounded once to y_dtype, or quantized from binary32 to MX
+ *
+ * quest_rmsnorm_fwd
+ *   x, residual      [rows x cols], dtype, row strides ldx, ldr; residual may be NULL
+ *   weight           [cols], w_dtype
+ *   eps              finite, >= 0
+ *   h                device out, dense, dtype; required with a residual, ignored without
+ *   rstd             device out [rows] binary32, or NULL
+ *   y, y_dtype       device out, dense; NULL if mx_bits is not 0
+ *   mx_bits          0: y.  4 or 8: yq, sy as quest_quantize_mx(y) in that many bits with had_block (1 or 32) writes them; then
+ *                    cols is a multiple of 32 and every row of x, residual and h starts on a 16-byte boundary, and yq does
+ *   1 <= cols <= 16384, 0 <= rows <= 2^24.  Without MX output no alignment beyond that of an element is asked for (rows on
+ *   16-byte boundaries are faster).
+ *
+ * quest_rmsnorm_bwd -- with n = h rstd and g = dy weight:
+ *     dx = dres + rstd (g - n mean(g n)),   dw = sum over rows of dy n
+ *   dx is the gradient of x and of the residual alike.  dy, h, dres (may be NULL): dtype, row strides lddy, ldh, lddr;
+ *   rstd: what the forward call wrote; dx device out, dense, dtype; dw device out [cols] binary32, summed in a fixed order; either
+ *   may be NULL.  workspace: quest_rmsnorm_bwd_workspace_bytes(rows, cols) bytes, 256-byte aligned.
+ */
+int quest_rmsnorm_fwd(const void *x, const void *residual, int dtype, int64_t ldx, int64_t ldr, const void *weight, int w_dtype,
+                      int64_t rows, int64_t cols, float eps, void *h, float *rstd, void *y, int y_dtype,
+                      int mx_bits, int had_block, uint8_t *yq, uint8_t *sy, void *stream);
+int quest_rmsnorm_bwd(const void *dy, const void *h, const void *dres, int dtype, int64_t lddy, int64_t ldh, int64_t lddr,
+                      const void *weight, int w_dtype, const float *rstd, int64_t rows, int64_t cols,
+                      void *dx, float *dw, void *workspace, size_t workspace_bytes, void *stream);
+size_t quest_rmsnorm_bwd_workspace_bytes(int64_t rows, int64_t cols);
 
 /* Bytes of scratch quest_lowbit_gemm / quest_linear_fwd need (0 on invalid arguments). */
 size_t quest_workspace_bytes(int64_t M, int64_t N, int64_t K, int bits_x, int bits_w);

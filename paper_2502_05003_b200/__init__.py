@@ -490,3 +490,331 @@ def quest_linear_fwd_fp4(x: torch.Tensor, w: torch.Tensor, had_block: int, trust
         1 if w_cached is not None else 0, _p(workspace), workspace.numel() if workspace is not None else 0, _stream()))
     out["y"] = y
     return out
+
+
+# ---- microscaled (MX) layer: a power-of-two scale for every 32 elements; weights in 4 bits, activations in 4 or 8 -------
+
+_MX_BLOCK = 32
+
+
+def quest_mx_scales_bytes(rows: int, cols: int) -> int:
+    """Bytes of the scales of an MX tensor (0 for a shape that the calls do not take)."""
+    return int(_lib.load().quest_mx_scales_bytes(rows, cols))
+
+
+def mx_scales_tiled(scales: torch.Tensor) -> torch.Tensor:
+    """Scale bytes as checkpoints hold them, [rows, cols / 32], in the order that the calls take."""
+    rows, blocks = scales.shape
+    room = torch.zeros((-(-rows // 128) * 128, -(-blocks // 4) * 4), dtype=torch.uint8, device=scales.device)
+    room[:rows, :blocks] = scales
+    return room.reshape(-1, 4, 32, room.shape[1] // 4, 4).permute(0, 3, 2, 1, 4).reshape(-1).contiguous()
+
+
+def mx_scales_rows(scales: torch.Tensor, rows: int, cols: int) -> torch.Tensor:
+    """The inverse of ``mx_scales_tiled``: [rows, cols / 32]."""
+    tiles = -(-cols // 128)
+    n = -(-rows // 128) * tiles * 512
+    t = scales.reshape(-1)[:n].reshape(-1, tiles, 32, 4, 4).permute(0, 3, 2, 1, 4)
+    return t.reshape(t.shape[0] * 128, tiles * 4)[:rows, :cols // _MX_BLOCK].contiguous()
+
+
+def _beside(name: str, x: torch.Tensor, **tensors):
+    """x and every tensor that is given are in the memory of one CUDA device."""
+    _require_cuda(x, *tensors.values())
+    for key, t in tensors.items():
+        if t is not None and t.device != x.device:
+            raise ValueError(f"{name}: {key} is on another device")
+
+
+def _rows_of(name: str, key: str, t: torch.Tensor, shape=None):
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{name}: {key} must be 2-D with unit inner stride")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: {key} must have the shape {tuple(shape)}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _kept(name: str, out: dict, key: str, shape, dtype, device):
+    """The tensor under ``key``, which must have that type and room for the shape, or a new one."""
+    t = out.get(key)
+    if t is None:
+        t = out[key] = torch.empty(shape, dtype=dtype, device=device)
+        return t
+    n = 1
+    for v in shape:
+        n *= v
+    if t.device != device or t.dtype != dtype or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{name}: {key} must be a contiguous {dtype} tensor on {device} with {n} elements")
+    return t
+
+
+def _mx_codes_of(name: str, key: str, t: torch.Tensor, cols: int, bits: int):
+    if t.dtype != torch.uint8 or t.dim() != 2 or not t.is_contiguous() or t.shape[1] * 8 != cols * bits:
+        raise ValueError(f"{name}: {key} must be a contiguous uint8 tensor [rows, {cols * bits // 8}]")
+
+
+def _mx_scales_of(name: str, key: str, t: torch.Tensor, rows: int, cols: int):
+    if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() < quest_mx_scales_bytes(rows, cols):
+        raise ValueError(f"{name}: {key} must be a contiguous uint8 tensor of {quest_mx_scales_bytes(rows, cols)} bytes")
+
+
+def _product_out(name: str, y, M: int, N: int, out_dtype, device):
+    if y is None:
+        return torch.empty((M, N), dtype=out_dtype, device=device), max(N, 1)
+    return y, _rows_of(name, "y", y, (M, N))
+
+
+def _mx_check(name: str, bits: int):
+    if bits not in (4, 8):
+        raise ValueError(f"{name}: 4 or 8 bits")
+
+
+def quest_quantize_mx(x: torch.Tensor, bits: int, had_block: int = 1, codes: torch.Tensor = None, scales: torch.Tensor = None):
+    """Rows of ``x`` [rows, cols] -> (codes uint8 [rows, cols * bits / 8], scales uint8 [quest_mx_scales_bytes]).  ``bits``: 4
+    (E2M1) or 8 (E4M3, ``codes.view(torch.float8_e4m3fn)``); ``had_block``: 1, or 32 for rotated blocks."""
+    done = _lib.binding().quantize_mx(x, bits, had_block, codes, scales)
+    if done is not None:
+        return _result(done)
+    name = "quest_quantize_mx"
+    _beside(name, x, codes=codes, scales=scales)
+    _mx_check(name, bits)
+    ld, (rows, cols) = _rows_of(name, "x", x), x.shape
+    out = {"codes": codes, "scales": scales}
+    codes = _kept(name, out, "codes", (rows, cols * bits // 8), torch.uint8, x.device)
+    scales = _kept(name, out, "scales", (quest_mx_scales_bytes(rows, cols),), torch.uint8, x.device)
+    with torch.cuda.device(x.device):
+        _lib.check(_lib.load().quest_quantize_mx(_p(x), _dtype_code(x), rows, cols, ld, bits, had_block, _p(codes), _p(scales), _stream()))
+    return codes, scales
+
+
+def quest_dequantize_mx(codes: torch.Tensor, scales: torch.Tensor, bits: int, out_dtype=torch.bfloat16, out: torch.Tensor = None):
+    """Values [rows, cols] of an MX tensor, exact in binary32 and (down to 2^-133) in bfloat16; rotated where x was rotated."""
+    done = _lib.binding().dequantize_mx(codes, scales, bits, out_dtype, out)
+    if done is not None:
+        return _result(done)
+    name = "quest_dequantize_mx"
+    _beside(name, codes, scales=scales, out=out)
+    _mx_check(name, bits)
+    if codes.dim() != 2:
+        raise ValueError(f"{name}: codes must be 2-D")
+    rows, cols = codes.shape[0], codes.shape[1] * 8 // bits
+    _mx_codes_of(name, "codes", codes, cols, bits)
+    _mx_scales_of(name, "scales", scales, rows, cols)
+    out = _kept(name, {"out": out}, "out", (rows, cols), out_dtype if out is None else out.dtype, codes.device)
+    with torch.cuda.device(codes.device):
+        _lib.check(_lib.load().quest_dequantize_mx(_p(codes), _p(scales), rows, cols, bits, _p(out), _dtype_code(out), _stream()))
+    return out
+
+
+def quest_gemm_mx(xq: torch.Tensor, sx: torch.Tensor, bits_x: int, wq: torch.Tensor, sw: torch.Tensor, K: int,
+                  out_dtype=torch.bfloat16, y: torch.Tensor = None) -> torch.Tensor:
+    """y [M, N] = x w^T of two MX tensors: x in 4 or 8 bits, w in 4.  K a multiple of 32, of 128 where x has 8 bits."""
+    done = _lib.binding().gemm_mx(xq, sx, bits_x, wq, sw, K, out_dtype, y)
+    if done is not None:
+        return _result(done)
+    name = "quest_gemm_mx"
+    _beside(name, xq, sx=sx, wq=wq, sw=sw, y=y)
+    _mx_check(name, bits_x)
+    _mx_codes_of(name, "xq", xq, K, bits_x)
+    _mx_codes_of(name, "wq", wq, K, 4)
+    M, N = xq.shape[0], wq.shape[0]
+    _mx_scales_of(name, "sx", sx, M, K)
+    _mx_scales_of(name, "sw", sw, N, K)
+    with torch.cuda.device(xq.device):
+        y, ldy = _product_out(name, y, M, N, out_dtype, xq.device)
+        _lib.check(_lib.load().quest_gemm_mx(_p(xq), _p(sx), bits_x, _p(wq), _p(sw), M, N, K, _p(y), _dtype_code(y), ldy, _stream()))
+    return y
+
+
+def quest_linear_fwd_mx(x: torch.Tensor, w: torch.Tensor, bits_x: int = 8, had_block: int = 1, out_dtype=None,
+                        y: torch.Tensor = None, saved: dict = None, w_cached: dict = None, want_codes: bool = True) -> dict:
+    """The microscaled layer, y = x w^T with x in ``bits_x`` bits and w in 4: returns {"y", "xq", "sx", "wq", "sw"}.
+
+    ``saved`` may carry preallocated tensors under those keys; ``w_cached`` = {"wq", "sw"} holds weights that are quantized
+    already (then ``w`` may be None).  With ``want_codes`` false up to 32 rows of x are quantized inside the product and
+    their codes are not stored (None); more rows need the room all the same.  ``x`` or ``w`` whose rows do not start on
+    16-byte boundaries, or with another inner stride, is copied first."""
+    done = _lib.binding().linear_fwd_mx(x, w, bits_x, had_block, out_dtype, y, saved, w_cached, want_codes)
+    if done is not None:
+        return _result(done)
+    name = "quest_linear_fwd_mx"
+    out = dict(saved or {})
+    if w_cached is not None:
+        out["wq"], out["sw"], w = w_cached["wq"], w_cached["sw"], None
+    _beside(name, x, w=w, y=y, **{k: out.get(k) for k in ("xq", "sx", "wq", "sw")})
+    _mx_check(name, bits_x)
+
+    def rows(key, t):
+        if t.dim() != 2:
+            raise ValueError(f"{name}: {key} must be 2-D")
+        if t.stride(1) != 1 or t.stride(0) < t.shape[1] or t.data_ptr() % 16 or t.stride(0) * t.element_size() % 16:
+            t = t.contiguous()
+        if t.data_ptr() % 16:
+            t = t.clone()
+        return t, max(t.stride(0), t.shape[1])
+
+    x, ldx = rows("x", x)
+    M, K = x.shape
+    dev = x.device
+    with torch.cuda.device(dev):
+        if w_cached is None:
+            w, ldw = rows("w", w)
+            N = w.shape[0]
+            if w.shape[1] != K:
+                raise ValueError(f"{name}: x [M, K] and w [N, K]")
+            wdt = _dtype_code(w)
+        else:
+            _mx_codes_of(name, "wq", out["wq"], K, 4)
+            N, ldw, wdt = out["wq"].shape[0], K, BF16
+            _mx_scales_of(name, "sw", out["sw"], N, K)
+        _kept(name, out, "wq", (N, K // 2), torch.uint8, dev)
+        _kept(name, out, "sw", (quest_mx_scales_bytes(N, K),), torch.uint8, dev)
+        if want_codes or M > 32:
+            _kept(name, out, "xq", (M, K * bits_x // 8), torch.uint8, dev)
+            _kept(name, out, "sx", (quest_mx_scales_bytes(M, K),), torch.uint8, dev)
+        else:
+            out["xq"] = out["sx"] = None
+        y, ldy = _product_out(name, y, M, N, out_dtype or x.dtype, dev)
+        _lib.check(_lib.load().quest_linear_fwd_mx(
+            _p(x), _dtype_code(x), ldx, _p(w), wdt, ldw, M, N, K, bits_x, had_block, _p(y), _dtype_code(y), ldy,
+            _p(out["xq"]), _p(out["sx"]), _p(out["wq"]), _p(out["sw"]), 0 if w_cached is None else 1, _stream()))
+    out["y"] = y
+    return out
+
+
+def quest_bwd_mx_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(_lib.load().quest_bwd_mx_workspace_bytes(M, N, K))
+
+
+def quest_linear_bwd_mx(dy: torch.Tensor, fwd: dict, bits_x: int, had_block: int, K: int, out_dtype=torch.float32,
+                        dx: torch.Tensor = None, dw: torch.Tensor = None, want_dx: bool = True, want_dw: bool = True,
+                        workspace: torch.Tensor = None) -> dict:
+    """Gradients of ``quest_linear_fwd_mx`` straight through the rounding, from what it returned (xq, sx for dw; wq, sw for
+    dx).  ``dy`` [M, N] bfloat16, dense.  Returns {"dx": [M, K] or None, "dw": [N, K] or None}; both have one type."""
+    done = _lib.binding().linear_bwd_mx(dy, fwd, bits_x, had_block, K, out_dtype, dx, dw, want_dx, want_dw, workspace)
+    if done is not None:
+        return _result(done)
+    name = "quest_linear_bwd_mx"
+    want_dx, want_dw = want_dx or dx is not None, want_dw or dw is not None
+    used = (["xq", "sx"] if want_dw else []) + (["wq", "sw"] if want_dx else [])
+    _beside(name, dy, dx=dx, dw=dw, workspace=workspace, **{k: fwd.get(k) for k in used})
+    _mx_check(name, bits_x)
+    if dy.dtype != torch.bfloat16 or dy.dim() != 2 or not dy.is_contiguous():
+        raise ValueError(f"{name}: dy must be a contiguous bfloat16 matrix")
+    M, N = dy.shape
+    n = quest_bwd_mx_workspace_bytes(M, N, K)
+    if n == 0:
+        raise ValueError(f"{name}: unsupported shape (M, N multiples of 8; K a multiple of 32, <= 16384)")
+    for key in used:
+        t, rows = fwd.get(key), M if key in ("xq", "sx") else N
+        if t is None:
+            raise ValueError(f"{name}: {key} of the forward call is missing")
+        if key in ("xq", "wq"):
+            _mx_codes_of(name, key, t, K, bits_x if key == "xq" else 4)
+            if t.shape[0] != rows:
+                raise ValueError(f"{name}: {key} must have {rows} rows")
+        else:
+            _mx_scales_of(name, key, t, rows, K)
+    out = {"dx": dx, "dw": dw}
+    given = dx if dx is not None else dw
+    dt = out_dtype if given is None else given.dtype
+    with torch.cuda.device(dy.device):
+        if want_dx:
+            _kept(name, out, "dx", (M, K), dt, dy.device)
+        if want_dw:
+            _kept(name, out, "dw", (N, K), dt, dy.device)
+        if workspace is None:
+            workspace = torch.empty(n, dtype=torch.uint8, device=dy.device)
+        some = out["dx"] if out["dx"] is not None else out["dw"]
+        _lib.check(_lib.load().quest_linear_bwd_mx(
+            _p(dy), M, N, K, bits_x, had_block, *[_p(fwd[k]) if k in used else None for k in ("xq", "sx", "wq", "sw")],
+            _p(out["dx"]), _p(out["dw"]), _dtype_code(some) if some is not None else F32, _p(workspace),
+            workspace.numel() * workspace.element_size(), _stream()))
+    return out
+
+
+# ---- root-mean-square norm in front of a layer -------------------------------------------------------------------------
+
+def quest_rmsnorm_fwd(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual: torch.Tensor = None, out_dtype=None,
+                      mx_bits: int = None, had_block: int = 1, out: dict = None, want_rstd: bool = True) -> dict:
+    """h = x + residual, y = h (mean(h^2) + eps)^(-1/2) weight for every row.  Returns {"h" (None without a residual),
+    "rstd" [rows] or None, and "y" or, with ``mx_bits`` 4 or 8, "yq", "sy": the codes and scales that ``quest_gemm_mx``
+    takes}.  ``out`` may hold preallocated tensors under those keys."""
+    done = _lib.binding().rmsnorm_fwd(x, weight, eps, residual, out_dtype, mx_bits, had_block, out, want_rstd)
+    if done is not None:
+        return _result(done)
+    name = "quest_rmsnorm_fwd"
+    out = dict(out or {})
+    _beside(name, x, weight=weight, residual=residual, **{k: out.get(k) for k in ("h", "rstd", "y", "yq", "sy")})
+    ldx, (rows, cols) = _rows_of(name, "x", x), x.shape
+    if tuple(weight.shape) != (cols,) or not weight.is_contiguous():
+        raise ValueError(f"{name}: weight must be a contiguous vector of {cols} elements")
+    ldr = cols
+    if residual is not None:
+        ldr = _rows_of(name, "residual", residual, x.shape)
+        if residual.dtype != x.dtype:
+            raise TypeError(f"{name}: x and residual share one dtype")
+    if mx_bits is not None:
+        _mx_check(name, mx_bits)
+    with torch.cuda.device(x.device):
+        if residual is not None:
+            _kept(name, out, "h", (rows, cols), x.dtype, x.device)
+        else:
+            out["h"] = None
+        if want_rstd or out.get("rstd") is not None:
+            _kept(name, out, "rstd", (rows,), torch.float32, x.device)
+        else:
+            out["rstd"] = None
+        ydt = F32
+        if mx_bits is not None:
+            _kept(name, out, "yq", (rows, cols * mx_bits // 8), torch.uint8, x.device)
+            _kept(name, out, "sy", (quest_mx_scales_bytes(rows, cols),), torch.uint8, x.device)
+        else:
+            dt = out["y"].dtype if out.get("y") is not None else out_dtype or x.dtype
+            ydt = _dtype_code(_kept(name, out, "y", (rows, cols), dt, x.device))
+        _lib.check(_lib.load().quest_rmsnorm_fwd(
+            _p(x), _p(residual), _dtype_code(x), ldx, ldr, _p(weight), _dtype_code(weight), rows, cols, ctypes.c_float(eps),
+            _p(out["h"]), _p(out["rstd"]), _p(out["y"]) if mx_bits is None else None, ydt, mx_bits or 0, had_block,
+            _p(out["yq"]) if mx_bits else None, _p(out["sy"]) if mx_bits else None, _stream()))
+    return out
+
+
+def quest_rmsnorm_bwd_workspace_bytes(rows: int, cols: int) -> int:
+    return int(_lib.load().quest_rmsnorm_bwd_workspace_bytes(rows, cols))
+
+
+def quest_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, dres: torch.Tensor = None,
+                      out: dict = None, want_dx: bool = True, want_dw: bool = True, workspace: torch.Tensor = None) -> dict:
+    """Gradient of ``quest_rmsnorm_fwd``: ``h`` is what was normalised (the forward call's "h", or x without a residual),
+    ``dres`` the gradient that reaches h on the residual stream.  Returns {"dx": the gradient of x and of the residual, "dw":
+    float32 [cols]}; ``out`` may hold preallocated tensors under those keys."""
+    done = _lib.binding().rmsnorm_bwd(dy, h, weight, rstd, dres, out, want_dx, want_dw, workspace)
+    if done is not None:
+        return _result(done)
+    name = "quest_rmsnorm_bwd"
+    out = dict(out or {})
+    _beside(name, dy, h=h, weight=weight, rstd=rstd, dres=dres, workspace=workspace, **{k: out.get(k) for k in ("dx", "dw")})
+    lddy, (rows, cols) = _rows_of(name, "dy", dy), dy.shape
+    ldh, lddr = _rows_of(name, "h", h, dy.shape), cols
+    if dres is not None:
+        lddr = _rows_of(name, "dres", dres, dy.shape)
+    if h.dtype != dy.dtype or (dres is not None and dres.dtype != dy.dtype):
+        raise TypeError(f"{name}: dy, h and dres share one dtype")
+    if tuple(weight.shape) != (cols,) or not weight.is_contiguous():
+        raise ValueError(f"{name}: weight must be a contiguous vector of {cols} elements")
+    if rstd.dtype != torch.float32 or not rstd.is_contiguous() or rstd.numel() < rows:
+        raise ValueError(f"{name}: rstd must be a contiguous float32 tensor of {rows} elements")
+    want_dx, want_dw = want_dx or out.get("dx") is not None, want_dw or out.get("dw") is not None
+    with torch.cuda.device(dy.device):
+        for key, wanted, shape, dt in (("dx", want_dx, (rows, cols), dy.dtype), ("dw", want_dw, (cols,), torch.float32)):
+            if wanted:
+                _kept(name, out, key, shape, dt, dy.device)
+            else:
+                out[key] = None
+        if workspace is None and want_dw:
+            workspace = torch.empty(quest_rmsnorm_bwd_workspace_bytes(rows, cols), dtype=torch.uint8, device=dy.device)
+        _lib.check(_lib.load().quest_rmsnorm_bwd(
+            _p(dy), _p(h), _p(dres), _dtype_code(dy), lddy, ldh, lddr, _p(weight), _dtype_code(weight), _p(rstd), rows, cols,
+            _p(out["dx"]), _p(out["dw"]), _p(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0,
+            _stream()))
+    return out

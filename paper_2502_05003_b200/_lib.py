@@ -18,6 +18,9 @@ EXPORTS = (
     "quest_linear_fwd_weight_only", "quest_weight_only_workspace_bytes",
     "quest_mlp_fwd", "quest_mlp_workspace_bytes", "quest_linear_fwd_quantize", "quest_linear_fwd_contract",
     "quest_selftest_bounded_wait",
+    "quest_mx_scales_bytes", "quest_quantize_mx", "quest_dequantize_mx", "quest_gemm_mx", "quest_linear_fwd_mx",
+    "quest_linear_bwd_mx", "quest_bwd_mx_workspace_bytes",
+    "quest_rmsnorm_fwd", "quest_rmsnorm_bwd", "quest_rmsnorm_bwd_workspace_bytes",
 )
 
 _lib = None
@@ -78,6 +81,26 @@ def load() -> ctypes.CDLL:
     L.quest_mlp_fwd.argtypes = [vp, vp, vp, vp, ci, i64, i64, i64, ci, ci, cf, vp, vp, ci, vp, vp, sz, vp]
     L.quest_mlp_workspace_bytes.restype = sz
     L.quest_mlp_workspace_bytes.argtypes = [i64, i64, i64]
+    L.quest_mx_scales_bytes.restype = sz
+    L.quest_mx_scales_bytes.argtypes = [i64, i64]
+    L.quest_quantize_mx.restype = ci
+    L.quest_quantize_mx.argtypes = [vp, ci, i64, i64, i64, ci, ci, vp, vp, vp]
+    L.quest_dequantize_mx.restype = ci
+    L.quest_dequantize_mx.argtypes = [vp, vp, i64, i64, ci, vp, ci, vp]
+    L.quest_gemm_mx.restype = ci
+    L.quest_gemm_mx.argtypes = [vp, vp, ci, vp, vp, i64, i64, i64, vp, ci, i64, vp]
+    L.quest_linear_fwd_mx.restype = ci
+    L.quest_linear_fwd_mx.argtypes = [vp, ci, i64, vp, ci, i64, i64, i64, i64, ci, ci, vp, ci, i64, vp, vp, vp, vp, ci, vp]
+    L.quest_linear_bwd_mx.restype = ci
+    L.quest_linear_bwd_mx.argtypes = [vp, i64, i64, i64, ci, ci, vp, vp, vp, vp, vp, vp, ci, vp, sz, vp]
+    L.quest_bwd_mx_workspace_bytes.restype = sz
+    L.quest_bwd_mx_workspace_bytes.argtypes = [i64, i64, i64]
+    L.quest_rmsnorm_fwd.restype = ci
+    L.quest_rmsnorm_fwd.argtypes = [vp, vp, ci, i64, i64, vp, ci, i64, i64, cf, vp, vp, vp, ci, ci, ci, vp, vp, vp]
+    L.quest_rmsnorm_bwd.restype = ci
+    L.quest_rmsnorm_bwd.argtypes = [vp, vp, vp, ci, i64, i64, i64, vp, ci, vp, i64, i64, vp, vp, vp, sz, vp]
+    L.quest_rmsnorm_bwd_workspace_bytes.restype = sz
+    L.quest_rmsnorm_bwd_workspace_bytes.argtypes = [i64, i64]
     L.quest_workspace_bytes.restype = sz
     L.quest_workspace_bytes.argtypes = [i64, i64, i64, ci, ci]
     L.quest_codes_bytes.restype = sz

@@ -1,8 +1,8 @@
 """Builds the CUDA library in-tree: ``python -m paper_2502_05003_b200.build``.
 
-nvcc cross-compiles for sm_100a without a GPU.  The quantizer is compiled with ``-fmad=false``
-(its binary32 operation order is part of the contract), and so is the decoding layer that repeats it; everything
-else with defaults.
+nvcc cross-compiles for sm_100a without a GPU.  The quantizers are compiled with ``-fmad=false``
+(their binary32 operation order is part of the contract), and so are the decoding layers that repeat it and the norm;
+everything else with defaults.
 """
 from __future__ import annotations
 
@@ -29,6 +29,10 @@ UNITS = {
     "quest_static.cu": [],
     "quest_backward.cu": [],
     "quest_weight_only.cu": [],
+    "quest_mx.cu": ["-fmad=false"],
+    "quest_mx_decode.cu": ["-fmad=false"],
+    "quest_mx_gemm.cu": [],
+    "quest_norm.cu": ["-fmad=false"],
 }
 
 

@@ -20,6 +20,7 @@
 #include <math.h>
 
 #include "quest_internal.cuh"
+#include "quest_mx.cuh"
 
 namespace quest {
 namespace {
@@ -330,6 +331,7 @@ iht_wide_kernel(const float *__restrict__ d, long long rows, int cols, float inv
 struct BwdWorkspace {
     uint16_t *wh, *xh;      // dequantised operands [N x K], [M x K]
     float *d1, *d2;         // masked products when the inverse transform is a separate kernel
+    size_t d_bytes;         // from d1 to the end of d2
     size_t bytes;
 };
 BwdWorkspace carve_bwd(void *base, int64_t M, int64_t N, int64_t K) {
@@ -339,8 +341,10 @@ BwdWorkspace carve_bwd(void *base, int64_t M, int64_t N, int64_t K) {
     auto take = [&](size_t n) { uint8_t *p = b + off; off += align_up(n, 256); return p; };
     w.wh = reinterpret_cast<uint16_t *>(take((size_t)N * K * 2));
     w.xh = reinterpret_cast<uint16_t *>(take((size_t)M * K * 2));
+    const size_t before = off;
     w.d1 = reinterpret_cast<float *>(take((size_t)M * K * 4));
     w.d2 = reinterpret_cast<float *>(take((size_t)N * K * 4));
+    w.d_bytes = off - before;
     w.bytes = off;
     return w;
 }
@@ -448,6 +452,30 @@ bool bwd_shape_ok(int64_t M, int64_t N, int64_t K) {
            M <= ((int64_t)1 << 24) && N <= ((int64_t)1 << 24);
 }
 
+struct Stage {                                   // RAII bracket for quest_stage_timing
+    void *h;
+    Stage(int id, cudaStream_t s_) : h(stage_begin(id, s_)) {}
+    ~Stage() { stage_end(h); }
+};
+
+// One gradient [I x K]: masked product of a and b over Kc terms (see launch_gemm_bf16_masked), then the inverse transform.
+// Blocks of up to 128 in rows of whole 128-column groups: the inverse transform runs in the contraction's epilogue, the masked
+// product never reaches memory.
+int masked_gradient(const BwdWorkspace &ws, const void *a, const void *b, int64_t I, int64_t Kc, int64_t K, const uint8_t *mask,
+                    int had_block, void *out, int out_dtype, float *d, int opl, cudaStream_t st) {
+    Stage gemm_stage(QUEST_STAGE_GEMM, st);
+    const bool fuse = had_block <= 128 && K % 128 == 0;
+    const int64_t rows_free = (int64_t)ws.d_bytes / (K * 4);
+    const int parts = transform_adds_parts(K, had_block) ? divide_contraction(I, K, Kc, rows_free, fuse) : 1;
+    if (parts > 1) {                                 // the products run one after the other: both may use d1 and d2
+        const int e = launch_gemm_bf16_parts(a, b, I, K, Kc, ws.d1, parts, opl, st);
+        return e ? e : launch_iht(ws.d1, I, K, had_block, out, out_dtype, parts, mask, st);
+    }
+    if (fuse) return launch_gemm_bf16_masked(a, b, I, K, Kc, mask, out, out_dtype, had_block, opl, st);
+    const int e = launch_gemm_bf16_masked(a, b, I, K, Kc, mask, d, QUEST_F32, 0, opl, st);
+    return e ? e : launch_iht(d, I, K, had_block, out, out_dtype, 1, nullptr, st);
+}
+
 }  // namespace
 }  // namespace quest
 
@@ -480,11 +508,6 @@ extern "C" int quest_linear_bwd(const void *dy, int64_t M, int64_t N, int64_t K,
     if (s) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     BwdWorkspace ws = carve_bwd(workspace, M, N, K);
-    struct Stage {                                   // RAII bracket for quest_stage_timing
-        void *h;
-        Stage(int id, cudaStream_t s_) : h(stage_begin(id, s_)) {}
-        ~Stage() { stage_end(h); }
-    };
     {
         // both dequantised operands in one launch, then the two products back to back
         Stage prep(QUEST_STAGE_UNPACK, st);
@@ -515,25 +538,52 @@ extern "C" int quest_linear_bwd(const void *dy, int64_t M, int64_t N, int64_t K,
         }
         if (e != cudaSuccess) return cuda_fail(e);
     }
-    // blocks of up to 128 in rows of whole 128-column groups: the inverse transform runs in the contraction's epilogue,
-    // the masked product never reaches memory
-    const bool fuse = had_block <= 128 && K % 128 == 0;
-    // one gradient: masked product of a and b (see launch_gemm_bf16_masked), then the inverse transform
-    const int64_t rows_free = (int64_t)(((uint8_t *)workspace + ws.bytes - (uint8_t *)ws.d1) / (K * 4));
-    auto gradient = [&](const void *a, const void *b, int64_t I, int64_t Kc, const uint8_t *mask, void *out, float *d, int opl) {
-        Stage gemm_stage(QUEST_STAGE_GEMM, st);
-        const int parts = transform_adds_parts(K, had_block) ? divide_contraction(I, K, Kc, rows_free, fuse) : 1;
-        if (parts > 1) {                                     // the products run one after the other: both may use d1 and d2
-            const int e = launch_gemm_bf16_parts(a, b, I, K, Kc, ws.d1, parts, opl, st);
-            return e ? e : launch_iht(ws.d1, I, K, had_block, out, out_dtype, parts, mask, st);
-        }
-        if (fuse) return launch_gemm_bf16_masked(a, b, I, K, Kc, mask, out, out_dtype, had_block, opl, st);
-        const int e = launch_gemm_bf16_masked(a, b, I, K, Kc, mask, d, QUEST_F32, 0, opl, st);
-        return e ? e : launch_iht(d, I, K, had_block, out, out_dtype, 1, nullptr, st);
-    };
     // activation gradient of Algorithm 2 with its trust mask: d1[m][k] = M_x[m][k] * sum_n dy[m][n] wq_h[n][k]
-    if (dx && (s = gradient(dy, ws.wh, M, N, mx, dx, ws.d1, 1))) return s;
+    if (dx && (s = masked_gradient(ws, dy, ws.wh, M, N, K, mx, had_block, dx, out_dtype, ws.d1, 1, st))) return s;
     // weight gradient of Algorithm 2 with its trust mask: d2[n][k] = M_w[n][k] * sum_m dy[m][n] xq_h[m][k]
-    if (dw && (s = gradient(dy, ws.xh, N, M, mw, dw, ws.d2, 2))) return s;
+    if (dw && (s = masked_gradient(ws, dy, ws.xh, N, M, K, mw, had_block, dw, out_dtype, ws.d2, 2, st))) return s;
+    return QUEST_OK;
+}
+
+// The microscaled layer: the same two products on the values of MX tensors, straight through the rounding (every element
+// counts as trusted: the mask is all ones, written beside the values).
+extern "C" size_t quest_bwd_mx_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    if (!bwd_shape_ok(M, N, K)) return 0;
+    return carve_bwd(nullptr, M, N, K).bytes + align_up((size_t)(M * K / 8), 256) + align_up((size_t)(N * K / 8), 256);
+}
+
+extern "C" int quest_linear_bwd_mx(const void *dy, int64_t M, int64_t N, int64_t K, int bits_x, int had_block, const uint8_t *xq,
+                                   const uint8_t *sx, const uint8_t *wq, const uint8_t *sw, void *dx, void *dw, int out_dtype,
+                                   void *workspace, size_t workspace_bytes, void *stream) {
+    if (!dx && !dw) return QUEST_ERR_NULL;
+    if (!dy || (dw && (!xq || !sx)) || (dx && (!wq || !sw))) return QUEST_ERR_NULL;
+    if (!mx_bits_ok(bits_x)) return QUEST_ERR_BITS;
+    if (!bwd_shape_ok(M, N, K)) return QUEST_ERR_SHAPE;
+    if (!mx_had_ok(had_block)) return QUEST_ERR_HAD_BLOCK;
+    if (out_dtype != QUEST_F32 && out_dtype != QUEST_BF16) return QUEST_ERR_DTYPE;
+    auto al = [](const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; };
+    if (!al(dy, 16) || !al(xq, 16) || !al(wq, 16) || !al(dx, 16) || !al(dw, 16)) return QUEST_ERR_ALIGN;
+    if (!workspace || !al(workspace, 256) || workspace_bytes < quest_bwd_mx_workspace_bytes(M, N, K)) return QUEST_ERR_WORKSPACE;
+    int s = check_device();
+    if (s) return s;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const BwdWorkspace ws = carve_bwd(workspace, M, N, K);
+    uint8_t *ones_x = static_cast<uint8_t *>(workspace) + ws.bytes, *ones_w = ones_x + align_up((size_t)(M * K / 8), 256);
+    {
+        // the gradient of x takes the values of w and a mask of its own shape, and the other way round
+        Stage prep(QUEST_STAGE_UNPACK, st);
+        MxDequantJob jobs[2];
+        int n = 0;
+        if (dx) jobs[n++] = {wq, sw, N, ws.wh, dw ? ones_w : nullptr, 4};
+        if (dw) jobs[n++] = {xq, sx, M, ws.xh, dx ? ones_x : nullptr, bits_x};
+        if ((s = launch_mx_dequantize(jobs, n, QUEST_BF16, K, st))) return s;
+        // one gradient alone: its mask has the shape of the tensor that was not read
+        if (!dw || !dx) {
+            const cudaError_t e = cudaMemsetAsync(dx ? ones_x : ones_w, 0xFF, (size_t)((dx ? M : N) * K / 8), st);
+            if (e != cudaSuccess) return cuda_fail(e);
+        }
+    }
+    if (dx && (s = masked_gradient(ws, dy, ws.wh, M, N, K, ones_x, had_block, dx, out_dtype, ws.d1, 1, st))) return s;
+    if (dw && (s = masked_gradient(ws, dy, ws.xh, N, M, K, ones_w, had_block, dw, out_dtype, ws.d2, 2, st))) return s;
     return QUEST_OK;
 }

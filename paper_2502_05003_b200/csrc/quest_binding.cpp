@@ -12,6 +12,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
@@ -107,7 +108,7 @@ at::Tensor fresh(at::IntArrayRef shape, at::ScalarType t, const at::Device &dev)
 // Interned dictionary keys, made when the module is loaded.
 #define QUEST_KEYS(X) \
     X(xq) X(sx) X(mx) X(wq) X(sw) X(mw) X(y) X(xh) X(dx) X(dw) X(h) X(workspace) X(operand_in_workspace) \
-    X(wgq) X(swg) X(mwg) X(wuq) X(swu) X(mwu) X(hq) X(sh) X(mh) X(wdq) X(swd) X(mwd)
+    X(wgq) X(swg) X(mwg) X(wuq) X(swu) X(mwu) X(hq) X(sh) X(mh) X(wdq) X(swd) X(mwd) X(yq) X(sy) X(rstd)
 #define QUEST_KEY_DECLARE(name) PyObject *k_##name = nullptr;
 QUEST_KEYS(QUEST_KEY_DECLARE)
 PyObject *item(PyObject *dict, PyObject *key) {            // borrowed; NULL where missing
@@ -464,6 +465,330 @@ PyObject *mlp_fwd(PyObject *const *a) {
     return a[7];
 }
 
+// ---- microscaled layer and norm: everything on x's device, whichever is current ----
+
+// A tensor beside x: on its device.
+const at::Tensor &beside(PyObject *o, const at::Tensor &x) {
+    const at::Tensor &t = plain_tensor(o);
+    if (t.device() != x.device()) throw NotPlain();
+    return t;
+}
+const at::Tensor &rows_beside(PyObject *o, const at::Tensor &x) {        // a matrix with unit inner stride
+    const at::Tensor &t = beside(o, x);
+    if (t.dim() != 2 || t.stride(1) != 1 || t.stride(0) < t.size(1)) throw NotPlain();
+    return t;
+}
+void *room_beside(PyObject *o, const at::Tensor &x, at::ScalarType type, int64_t bytes) {
+    const at::Tensor &t = beside(o, x);
+    if (t.scalar_type() != type || !t.is_contiguous() || (int64_t)t.nbytes() < bytes) throw NotPlain();
+    return t.data_ptr();
+}
+int mx_bits_arg(PyObject *o) {
+    const int64_t b = int_arg(o);
+    if (b != 4 && b != 8) throw NotPlain();
+    return (int)b;
+}
+int64_t mx_scales(int64_t rows, int64_t cols) {
+    const int64_t n = (int64_t)quest_mx_scales_bytes(rows, cols);
+    if (!n) throw NotPlain();
+    return n;
+}
+bool on_16(const at::Tensor &t) {          // rows that the C ABI takes as they are
+    return reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0 && t.stride(0) * (int64_t)t.element_size() % 16 == 0;
+}
+// The tensor under a dictionary's key with room for `bytes`, or a new one that is put there; its memory.
+void *keep(Named &d, PyObject *key, const at::Tensor &x, at::IntArrayRef shape, at::ScalarType type) {
+    int64_t n = (int64_t)c10::elementSize(type);
+    for (const int64_t v : shape) n *= v;
+    if (PyObject *given = d.get(key)) return room_beside(given, x, type, n);
+    return d.need(key, shape, type);
+}
+
+// x, bits, had_block, codes, scales
+PyObject *quantize_mx(PyObject *const *a) {
+    const at::Tensor &x = rows_beside(a[0], plain_tensor(a[0]));
+    const int bits = mx_bits_arg(a[1]);
+    const int64_t g = int_arg(a[2]), rows = x.size(0), cols = x.size(1);
+    const int dt = code_of(x.scalar_type());
+    if (rows < 1) throw NotPlain();
+    const int64_t n = mx_scales(rows, cols);
+    c10::cuda::CUDAGuard guard(x.device());
+    auto out = [&](PyObject *o, at::IntArrayRef shape, int64_t bytes) {
+        if (o == Py_None) return THPVariable_Wrap(fresh(shape, at::kByte, x.device()));
+        room_beside(o, x, at::kByte, bytes);
+        Py_INCREF(o);
+        return o;
+    };
+    Ref codes(out(a[3], {rows, cols * bits / 8}, rows * cols * bits / 8)), scales(out(a[4], {n}, n));
+    void *cp = ptr(codes.p), *sp = ptr(scales.p), *st = stream();
+    const int s = unlocked([&] {
+        return quest_quantize_mx(x.data_ptr(), dt, rows, cols, x.stride(0), bits, (int)g, (uint8_t *)cp, (uint8_t *)sp, st);
+    });
+    if (s) return PyLong_FromLong(s);
+    return PyTuple_Pack(2, codes.p, scales.p);
+}
+
+// codes, scales, bits, out_dtype, out
+PyObject *dequantize_mx(PyObject *const *a) {
+    const at::Tensor &codes = rows_beside(a[0], plain_tensor(a[0]));
+    const int bits = mx_bits_arg(a[2]);
+    const int64_t rows = codes.size(0), cols = codes.size(1) * 8 / bits;
+    if (codes.scalar_type() != at::kByte || !codes.is_contiguous() || rows < 1) throw NotPlain();
+    const void *sp = room_beside(a[1], codes, at::kByte, mx_scales(rows, cols));
+    const at::ScalarType ot = a[4] == Py_None ? dtype_arg(a[3]) : beside(a[4], codes).scalar_type();
+    const int odt = code_of(ot);
+    c10::cuda::CUDAGuard guard(codes.device());
+    Ref out([&] {
+        if (a[4] == Py_None) return THPVariable_Wrap(fresh({rows, cols}, ot, codes.device()));
+        room_beside(a[4], codes, ot, rows * cols * (int64_t)c10::elementSize(ot));
+        Py_INCREF(a[4]);
+        return a[4];
+    }());
+    void *op = ptr(out.p), *st = stream();
+    const int s = unlocked([&] {
+        return quest_dequantize_mx((const uint8_t *)codes.data_ptr(), (const uint8_t *)sp, rows, cols, bits, op, odt, st);
+    });
+    if (s) return PyLong_FromLong(s);
+    return out.release();
+}
+
+// y of a product: given (any row stride, unit inner stride) or new
+at::Tensor product_out(PyObject *o, const at::Tensor &x, int64_t M, int64_t N, at::ScalarType ot) {
+    if (o == Py_None) return fresh({M, N}, ot, x.device());
+    const at::Tensor &y = rows_beside(o, x);
+    code_of(y.scalar_type());
+    if (y.size(0) != M || y.size(1) != N) throw NotPlain();
+    return y;
+}
+
+// xq, sx, bits_x, wq, sw, K, out_dtype, y
+PyObject *gemm_mx(PyObject *const *a) {
+    const at::Tensor &xq = rows_beside(a[0], plain_tensor(a[0])), &wq = rows_beside(a[3], xq);
+    const int bits = mx_bits_arg(a[2]);
+    const int64_t K = int_arg(a[5]), M = xq.size(0), N = wq.size(0);
+    if (M < 1 || N < 1 || xq.scalar_type() != at::kByte || wq.scalar_type() != at::kByte || !xq.is_contiguous() || !wq.is_contiguous() ||
+        xq.size(1) * 8 != K * bits || wq.size(1) * 2 != K)
+        throw NotPlain();
+    const void *sx = room_beside(a[1], xq, at::kByte, mx_scales(M, K)), *sw = room_beside(a[4], xq, at::kByte, mx_scales(N, K));
+    c10::cuda::CUDAGuard guard(xq.device());
+    const at::Tensor y = product_out(a[7], xq, M, N, a[7] == Py_None ? dtype_arg(a[6]) : at::kFloat);
+    const int ydt = code_of(y.scalar_type());
+    void *st = stream();
+    const int s = unlocked([&] {
+        return quest_gemm_mx((const uint8_t *)xq.data_ptr(), (const uint8_t *)sx, bits, (const uint8_t *)wq.data_ptr(), (const uint8_t *)sw,
+                             M, N, K, y.data_ptr(), ydt, y.stride(0), st);
+    });
+    if (s) return PyLong_FromLong(s);
+    if (a[7] != Py_None) { Py_INCREF(a[7]); return a[7]; }
+    return THPVariable_Wrap(y);
+}
+
+// x, w, bits_x, had_block, out_dtype, y, saved, w_cached, want_codes
+PyObject *linear_fwd_mx(PyObject *const *a) {
+    const at::Tensor &x = rows_beside(a[0], plain_tensor(a[0]));
+    const int bits = mx_bits_arg(a[2]);
+    const int64_t g = int_arg(a[3]), M = x.size(0), K = x.size(1);
+    const int xdt = code_of(x.scalar_type());
+    if (M < 1 || !on_16(x)) throw NotPlain();
+    Ref dict(copy_of_dict(a[6]));
+    Named out{dict.p, x.device()};
+    const bool cached = a[7] != Py_None, codes = bool_arg(a[8]);
+    const void *wp = nullptr;
+    int64_t N, ldw = K;
+    int wdt = QUEST_BF16;
+    c10::cuda::CUDAGuard guard(x.device());
+    if (cached) {
+        if (!PyDict_CheckExact(a[7])) throw NotPlain();
+        PyObject *wq = item(a[7], k_wq), *sw = item(a[7], k_sw);
+        if (!wq || !sw) throw NotPlain();
+        const at::Tensor &t = rows_beside(wq, x);
+        N = t.size(0);
+        if (t.size(1) * 2 != K) throw NotPlain();
+        out.set(k_wq, wq);
+        out.set(k_sw, sw);
+    } else {
+        const at::Tensor &w = rows_beside(a[1], x);
+        N = w.size(0);
+        if (w.size(1) != K || !on_16(w)) throw NotPlain();
+        wp = w.data_ptr();
+        ldw = w.stride(0);
+        wdt = code_of(w.scalar_type());
+    }
+    if (N < 1) throw NotPlain();
+    uint8_t *wq = (uint8_t *)keep(out, k_wq, x, {N, K / 2}, at::kByte), *sw = (uint8_t *)keep(out, k_sw, x, {mx_scales(N, K)}, at::kByte);
+    uint8_t *xq = nullptr, *sx = nullptr;
+    if (codes || M > 32) {
+        xq = (uint8_t *)keep(out, k_xq, x, {M, K * bits / 8}, at::kByte);
+        sx = (uint8_t *)keep(out, k_sx, x, {mx_scales(M, K)}, at::kByte);
+    } else {
+        out.set(k_xq, Py_None);
+        out.set(k_sx, Py_None);
+    }
+    const at::Tensor y = product_out(a[5], x, M, N, a[4] == Py_None ? x.scalar_type() : dtype_arg(a[4]));
+    const int ydt = code_of(y.scalar_type());
+    void *st = stream();
+    const int s = unlocked([&] {
+        return quest_linear_fwd_mx(x.data_ptr(), xdt, x.stride(0), wp, wdt, ldw, M, N, K, bits, (int)g, y.data_ptr(), ydt, y.stride(0), xq, sx,
+                                   wq, sw, cached ? 1 : 0, st);
+    });
+    if (s) return PyLong_FromLong(s);
+    if (a[5] != Py_None) {
+        out.set(k_y, a[5]);
+    } else {
+        Ref v(THPVariable_Wrap(y));
+        out.set(k_y, v.p);
+    }
+    return dict.release();
+}
+
+// dy, fwd, bits_x, had_block, K, out_dtype, dx, dw, want_dx, want_dw, workspace
+PyObject *linear_bwd_mx(PyObject *const *a) {
+    const at::Tensor &dy = dense(a[0]);
+    if (dy.scalar_type() != at::kBFloat16 || !PyDict_CheckExact(a[1])) throw NotPlain();
+    const int bits = mx_bits_arg(a[2]);
+    const int64_t g = int_arg(a[3]), K = int_arg(a[4]), M = dy.size(0), N = dy.size(1);
+    at::ScalarType ot = dtype_arg(a[5]);
+    const bool want_x = bool_arg(a[8]) || a[6] != Py_None, want_w = bool_arg(a[9]) || a[7] != Py_None;
+    const int64_t bytes = (int64_t)quest_bwd_mx_workspace_bytes(M, N, K);
+    if ((!want_x && !want_w) || !bytes) throw NotPlain();
+    auto saved = [&](PyObject *key, bool used, int64_t n) -> const uint8_t * {
+        if (!used) return nullptr;
+        PyObject *v = item(a[1], key);
+        if (!v) throw NotPlain();
+        return (const uint8_t *)room_beside(v, dy, at::kByte, n);
+    };
+    const uint8_t *xq = saved(k_xq, want_w, M * K * bits / 8), *sx = saved(k_sx, want_w, mx_scales(M, K));
+    const uint8_t *wq = saved(k_wq, want_x, N * K / 2), *sw = saved(k_sw, want_x, mx_scales(N, K));
+    c10::cuda::CUDAGuard guard(dy.device());
+    for (PyObject *o : {a[6], a[7]})
+        if (o != Py_None) ot = beside(o, dy).scalar_type();
+    const int odt = code_of(ot);
+    auto grad = [&](PyObject *o, bool wanted, int64_t rows) {
+        if (o != Py_None) {
+            room_beside(o, dy, ot, rows * K * (int64_t)c10::elementSize(ot));
+            Py_INCREF(o);
+            return o;
+        }
+        if (wanted) return THPVariable_Wrap(fresh({rows, K}, ot, dy.device()));
+        Py_INCREF(Py_None);
+        return Py_None;
+    };
+    Ref dx(grad(a[6], want_x, M)), dw(grad(a[7], want_w, N));
+    at::Tensor ws;
+    void *wsp;
+    int64_t wsn = bytes;
+    if (a[10] != Py_None) {
+        ws = beside(a[10], dy);
+        if (!ws.is_contiguous()) throw NotPlain();
+        wsn = (int64_t)ws.nbytes();
+    } else {
+        ws = fresh({bytes}, at::kByte, dy.device());
+    }
+    wsp = ws.data_ptr();
+    void *dxp = ptr(dx.p), *dwp = ptr(dw.p), *st = stream();
+    const int s = unlocked([&] {
+        return quest_linear_bwd_mx(dy.data_ptr(), M, N, K, bits, (int)g, xq, sx, wq, sw, dxp, dwp, odt, wsp, (size_t)wsn, st);
+    });
+    if (s) return PyLong_FromLong(s);
+    Ref d(PyDict_New());
+    Named out{d.p, dy.device()};
+    out.set(k_dx, dx.p);
+    out.set(k_dw, dw.p);
+    return d.release();
+}
+
+// x, weight, eps, residual, out_dtype, mx_bits, had_block, out, want_rstd
+PyObject *rmsnorm_fwd(PyObject *const *a) {
+    const at::Tensor &x = rows_beside(a[0], plain_tensor(a[0])), &weight = beside(a[1], x);
+    const int64_t rows = x.size(0), cols = x.size(1);
+    const float eps = float_arg(a[2]);
+    const int dt = code_of(x.scalar_type()), wdt = code_of(weight.scalar_type());
+    const int64_t g = int_arg(a[6]);
+    const bool rstd_wanted = bool_arg(a[8]);
+    const int bits = a[5] == Py_None ? 0 : mx_bits_arg(a[5]);
+    if (rows < 1 || weight.dim() != 1 || weight.size(0) != cols || !weight.is_contiguous()) throw NotPlain();
+    const void *res = nullptr;
+    int64_t ldr = cols;
+    if (a[3] != Py_None) {
+        const at::Tensor &r = rows_beside(a[3], x);
+        if (r.scalar_type() != x.scalar_type() || r.size(0) != rows || r.size(1) != cols) throw NotPlain();
+        res = r.data_ptr();
+        ldr = r.stride(0);
+    }
+    at::ScalarType ot = a[4] == Py_None ? x.scalar_type() : dtype_arg(a[4]);
+    c10::cuda::CUDAGuard guard(x.device());
+    Ref dict(copy_of_dict(a[7]));
+    Named out{dict.p, x.device()};
+    void *h = nullptr, *y = nullptr, *yq = nullptr, *sy = nullptr, *rstd = nullptr;
+    if (res) h = keep(out, k_h, x, {rows, cols}, x.scalar_type());
+    else out.set(k_h, Py_None);
+    if (rstd_wanted || out.get(k_rstd)) rstd = keep(out, k_rstd, x, {rows}, at::kFloat);
+    else out.set(k_rstd, Py_None);
+    if (bits) {
+        if (cols % 32) throw NotPlain();
+        yq = keep(out, k_yq, x, {rows, cols * bits / 8}, at::kByte);
+        sy = keep(out, k_sy, x, {mx_scales(rows, cols)}, at::kByte);
+    } else {
+        if (PyObject *given = out.get(k_y)) ot = beside(given, x).scalar_type();
+        code_of(ot);
+        y = keep(out, k_y, x, {rows, cols}, ot);
+    }
+    const int ydt = bits ? QUEST_F32 : code_of(ot);
+    void *st = stream();
+    const int s = unlocked([&] {
+        return quest_rmsnorm_fwd(x.data_ptr(), res, dt, x.stride(0), ldr, weight.data_ptr(), wdt, rows, cols, eps, h, (float *)rstd, y, ydt,
+                                 bits, (int)g, (uint8_t *)yq, (uint8_t *)sy, st);
+    });
+    if (s) return PyLong_FromLong(s);
+    return dict.release();
+}
+
+// dy, h, weight, rstd, dres, out, want_dx, want_dw, workspace
+PyObject *rmsnorm_bwd(PyObject *const *a) {
+    const at::Tensor &dy = rows_beside(a[0], plain_tensor(a[0])), &h = rows_beside(a[1], dy), &weight = beside(a[2], dy);
+    const int64_t rows = dy.size(0), cols = dy.size(1);
+    const int dt = code_of(dy.scalar_type()), wdt = code_of(weight.scalar_type());
+    if (rows < 1 || h.scalar_type() != dy.scalar_type() || h.sizes() != dy.sizes() || weight.dim() != 1 || weight.size(0) != cols ||
+        !weight.is_contiguous())
+        throw NotPlain();
+    const void *rstd = room_beside(a[3], dy, at::kFloat, 4 * rows), *dres = nullptr;
+    int64_t lddr = cols;
+    if (a[4] != Py_None) {
+        const at::Tensor &r = rows_beside(a[4], dy);
+        if (r.scalar_type() != dy.scalar_type() || r.sizes() != dy.sizes()) throw NotPlain();
+        dres = r.data_ptr();
+        lddr = r.stride(0);
+    }
+    c10::cuda::CUDAGuard guard(dy.device());
+    Ref dict(copy_of_dict(a[5]));
+    Named out{dict.p, dy.device()};
+    const bool want_x = bool_arg(a[6]) || out.get(k_dx), want_w = bool_arg(a[7]) || out.get(k_dw);
+    if (!want_x && !want_w) throw NotPlain();
+    void *dx = nullptr, *dw = nullptr, *wsp = nullptr;
+    int64_t wsn = 0;
+    if (want_x) dx = keep(out, k_dx, dy, {rows, cols}, dy.scalar_type());
+    else out.set(k_dx, Py_None);
+    if (want_w) dw = keep(out, k_dw, dy, {cols}, at::kFloat);
+    else out.set(k_dw, Py_None);
+    at::Tensor ws;
+    if (a[8] != Py_None) {
+        ws = beside(a[8], dy);
+        if (!ws.is_contiguous()) throw NotPlain();
+    } else if (want_w) {
+        const size_t n = quest_rmsnorm_bwd_workspace_bytes(rows, cols);
+        if (!n) throw NotPlain();
+        ws = fresh({(int64_t)n}, at::kByte, dy.device());
+    }
+    if (ws.defined()) { wsp = ws.data_ptr(); wsn = (int64_t)ws.nbytes(); }
+    void *st = stream();
+    const int s = unlocked([&] {
+        return quest_rmsnorm_bwd(dy.data_ptr(), h.data_ptr(), dres, dt, dy.stride(0), h.stride(0), lddr, weight.data_ptr(), wdt,
+                                 (const float *)rstd, rows, cols, dx, (float *)dw, wsp, (size_t)wsn, st);
+    });
+    if (s) return PyLong_FromLong(s);
+    return dict.release();
+}
+
 // QUEST_BINDING: the module's name (build.py: it carries the version of torch)
 #define QUEST_STRING_(X) #X
 #define QUEST_STRING(X) QUEST_STRING_(X)
@@ -473,6 +798,8 @@ PyObject *mlp_fwd(PyObject *const *a) {
 PyMethodDef methods[] = {
     QUEST_METHOD(quantize, 8), QUEST_METHOD(lowbit_gemm, 13), QUEST_METHOD(linear_fwd, 11), QUEST_METHOD(linear_bwd, 11),
     QUEST_METHOD(linear_fwd_fp4, 7), QUEST_METHOD(linear_fwd_weight_only, 8), QUEST_METHOD(mlp_fwd, 8),
+    QUEST_METHOD(quantize_mx, 5), QUEST_METHOD(dequantize_mx, 5), QUEST_METHOD(gemm_mx, 8), QUEST_METHOD(linear_fwd_mx, 9),
+    QUEST_METHOD(linear_bwd_mx, 11), QUEST_METHOD(rmsnorm_fwd, 9), QUEST_METHOD(rmsnorm_bwd, 9),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, QUEST_STRING(QUEST_BINDING), nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
