@@ -212,6 +212,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     } else if (warp == 1) {
         if (leader && elect_one()) {
             constexpr uint32_t idesc = make_idesc<XB>(TILE_M, BN);
+            const int num_whole = p.K / KB;
             int stage = 0, t = 0, slot = 0;
             uint32_t phase = 0;
             bool ok = true;
@@ -222,9 +223,12 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + (uint32_t)(buf * BN);
-                for (int kb = 0; kb < num_kb; ++kb) {
+                // one k-block: its scales, its products, the stage handed back.  instr: instructions of the block, fewer than four
+                // in a last one that ends behind K: there the operands are zero, but nothing says what the scale bytes of a group
+                // that no tile of the tensor has would hold
+                const auto block = [&](bool first, int instr) {
                     ok = mbar_wait(smem_u32(&full_bar[stage]), phase, abort_flag, p.status, ST_MMA);
-                    if (!ok) break;
+                    if (!ok) return;
                     tc_fence_after();
                     const uint32_t sa = smem_u32(ring + stage * L::STAGE_BYTES);
                     const uint32_t t_sfa = tmem_base + (uint32_t)(L::SF_COL + slot * L::SF_SLOT);
@@ -243,21 +247,20 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                     const uint64_t a_desc = make_smem_desc(sa), b_desc = make_smem_desc(sa + L::A_BYTES);
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk) {
-                        // the last stage stops behind K: beyond it the operands are zero, but nothing says what the scale bytes
-                        // of a group that no tile of the tensor has would hold
-                        if (kb * KB + kk * KI < p.K) {
-                            const int g = XB == 4 ? kk >> 1 : 0;
-                            const uint32_t sf = XB == 4 ? (uint32_t)(kk & 1) * 2 : (uint32_t)kk;
-                            umma_mx_pair<XB>(d_tmem, a_desc + (uint64_t)(kk * 2), b_desc + (uint64_t)(kk * 2),
-                                             idesc | (sf << 4) | (sf << 29), kb != 0 || kk != 0 ? 1u : 0u, t_sfa + 4 * g,
-                                             t_sfb + 4 * g * (BN / 128));
-                        }
+                        if (kk >= instr) break;
+                        const int g = XB == 4 ? kk >> 1 : 0;
+                        const uint32_t sf = XB == 4 ? (uint32_t)(kk & 1) * 2 : (uint32_t)kk;
+                        umma_mx_pair<XB>(d_tmem, a_desc + (uint64_t)(kk * 2), b_desc + (uint64_t)(kk * 2), idesc | (sf << 4) | (sf << 29),
+                                         first && kk == 0 ? 0u : 1u, t_sfa + 4 * g, t_sfb + 4 * g * (BN / 128));
                     }
                     umma_commit_pair(smem_u32(&empty_bar[stage]));
-                    slot = (slot + 1) % L::SF_SLOTS;
+                    slot = slot + 1 == L::SF_SLOTS ? 0 : slot + 1;
                     if (++stage == stages) { stage = 0; phase ^= 1u; }
-                }
-                if (ok) umma_commit_pair(smem_u32(&tfull_bar[buf]));
+                };
+                for (int kb = 0; kb < num_whole && ok; ++kb) block(kb == 0, 4);
+                if (ok && num_whole < num_kb) block(num_whole == 0, (p.K - num_whole * KB + KI - 1) / KI);
+                if (!ok) break;
+                umma_commit_pair(smem_u32(&tfull_bar[buf]));
             }
         }
         __syncwarp();
