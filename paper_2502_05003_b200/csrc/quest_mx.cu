@@ -249,7 +249,7 @@ int quest_linear_fwd_mx(const void *x, int x_dtype, int64_t ldx, const void *w, 
     if (!mx_had_ok(had_block)) return QUEST_ERR_HAD_BLOCK;
     if (M == 0 || N == 0) return QUEST_OK;
     const bool few = M <= MX_FEW_ROWS, keep = xq || sx;
-    if ((keep || !few) && (!xq || !sx)) return QUEST_ERR_NULL;
+    if ((keep || !mx_fuses_quantizer(M, K)) && (!xq || !sx)) return QUEST_ERR_NULL;
     if (keep && (!aligned(xq, 16) || !aligned(sx, 16))) return QUEST_ERR_ALIGN;
     if ((s = check_device())) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
