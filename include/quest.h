@@ -360,7 +360,7 @@ int quest_dequantize_mx(const uint8_t *codes, const uint8_t *scales, int64_t row
  *   xq, sx           device out: codes and scales of x, for a backward pass; both may be NULL where M <= 8 and M K <= 4096:
  *                    x is then quantized inside the product and nothing but y is written
  *   wq, sw           device out, or inputs with w_is_cached = 1 (w may be NULL then)
- * No workspace.  Errors as for quest_linear_fwd.
+ * No workspace.  Errors as for quest_linear_fwd.  M = 0 or N = 0: the operand that is not empty is quantized, nothing else is done.
  */
 int quest_gemm_mx(const uint8_t *xq, const uint8_t *sx, int bits_x, const uint8_t *wq, const uint8_t *sw,
                   int64_t M, int64_t N, int64_t K, void *y, int y_dtype, int64_t ldy_elems, void *stream);

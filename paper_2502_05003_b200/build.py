@@ -94,7 +94,7 @@ def build_binding(force: bool = False):
     for inc in includes:
         cmd += ["-isystem", inc]
     cmd += [src, "-o", tmp, "-L", HERE, "-l:libquest_b200.so", "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu",
-            "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"]
+            "-ltorch_cuda", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"]
     subprocess.check_call(cmd)
     os.replace(tmp, target)
     return target

@@ -4,6 +4,8 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <new>
+
 #include "quest_internal.cuh"
 #include "quest_operand.cuh"
 
@@ -105,7 +107,7 @@ struct StageScope {
 };
 
 // Stage brackets for translation units other than this one.
-void *stage_begin(int id, cudaStream_t st) { return new StageScope(id, st); }
+void *stage_begin(int id, cudaStream_t st) { return new (std::nothrow) StageScope(id, st); }       // NULL: not timed
 void stage_end(void *scope) { delete static_cast<StageScope *>(scope); }
 
 static bool is_pow2(int64_t v) { return v > 0 && (v & (v - 1)) == 0; }

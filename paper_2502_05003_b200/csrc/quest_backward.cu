@@ -471,6 +471,7 @@ int masked_gradient(const BwdWorkspace &ws, const void *a, const void *b, int64_
         const int e = launch_gemm_bf16_parts(a, b, I, K, Kc, ws.d1, parts, opl, st);
         return e ? e : launch_iht(ws.d1, I, K, had_block, out, out_dtype, parts, mask, st);
     }
+    if (had_block == 1 && out_dtype == QUEST_F32) return launch_gemm_bf16_masked(a, b, I, K, Kc, mask, out, QUEST_F32, 0, opl, st);
     if (fuse) return launch_gemm_bf16_masked(a, b, I, K, Kc, mask, out, out_dtype, had_block, opl, st);
     const int e = launch_gemm_bf16_masked(a, b, I, K, Kc, mask, d, QUEST_F32, 0, opl, st);
     return e ? e : launch_iht(d, I, K, had_block, out, out_dtype, 1, nullptr, st);

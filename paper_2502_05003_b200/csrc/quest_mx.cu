@@ -247,17 +247,19 @@ int quest_linear_fwd_mx(const void *x, int x_dtype, int64_t ldx, const void *w, 
     if ((s = check_rows(x, x_dtype, M, K, ldx))) return s;
     if (!w_is_cached && (s = check_rows(w, w_dtype, N, K, ldw))) return s;
     if (!mx_had_ok(had_block)) return QUEST_ERR_HAD_BLOCK;
-    if (M == 0 || N == 0) return QUEST_OK;
-    const bool few = M <= MX_FEW_ROWS, keep = xq || sx;
-    if ((keep || !mx_fuses_quantizer(M, K)) && (!xq || !sx)) return QUEST_ERR_NULL;
-    if (keep && (!aligned(xq, 16) || !aligned(sx, 16))) return QUEST_ERR_ALIGN;
+    // an empty product still quantizes the operand that there is
+    const bool few = M <= MX_FEW_ROWS, keep = M > 0 && (xq || sx), quantize_w = N > 0 && !w_is_cached;
+    if (quantize_w && (!wq || !sw)) return QUEST_ERR_NULL;
+    if ((keep || (M > 0 && N > 0 && !mx_fuses_quantizer(M, K))) && (!xq || !sx)) return QUEST_ERR_NULL;
+    if ((keep && (!aligned(xq, 16) || !aligned(sx, 16))) || (quantize_w && !aligned(wq, 16))) return QUEST_ERR_ALIGN;
+    if ((M == 0 || N == 0) && !keep && !quantize_w) return QUEST_OK;
     if ((s = check_device())) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     {
         MxJob jobs[2];
         int n = 0;
         if (keep) jobs[n++] = {x, M, ldx, xq, sx, bits_x};
-        if (!w_is_cached) jobs[n++] = {w, N, ldw, wq, sw, 4};
+        if (quantize_w) jobs[n++] = {w, N, ldw, wq, sw, 4};
         if (n) {
             void *h = stage_begin(keep ? QUEST_STAGE_QUANT_X : QUEST_STAGE_QUANT_W, st);
             if (n == 2 && x_dtype != w_dtype) {
@@ -270,6 +272,7 @@ int quest_linear_fwd_mx(const void *x, int x_dtype, int64_t ldx, const void *w, 
             if (s) return s;
         }
     }
+    if (M == 0 || N == 0) return QUEST_OK;
     void *h = stage_begin(QUEST_STAGE_GEMM, st);
     if (!few) s = launch_mx_gemm(xq, sx, bits_x, wq, sw, M, N, K, y, y_dtype, ldy_elems, st);
     else if (keep) s = launch_mx_few_rows(nullptr, 0, 0, xq, sx, bits_x, 1, wq, sw, M, N, K, y, y_dtype, ldy_elems, st);

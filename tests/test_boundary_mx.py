@@ -64,6 +64,8 @@ def test_linear(lib, change, status):
              ydt=0, ldy=64, cached=0) | change
     if a["K"] == 160:
         a["ldx"] = a["ldw"] = 160
+    if a["M"] == 0 or a["N"] == 0:
+        a |= dict(cached=1, xq=None, sx=None)              # nothing to quantize either
     assert lib.quest_linear_fwd_mx(a["x"], a["xdt"], a["ldx"], a["w"], a["wdt"], a["ldw"], a["M"], a["N"], a["K"], a["bits"], a["g"], a["y"],
                                    a["ydt"], a["ldy"], a["xq"], a["sx"], a["wq"], a["sw"], a["cached"], None) == status
 

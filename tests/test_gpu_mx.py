@@ -287,9 +287,13 @@ def test_empty_calls():
     c, s = quest.quest_quantize_mx(x, 8)
     assert c.shape == (0, 128) and s.numel() == 0
     assert quest.quest_dequantize_mx(c, s, 8).shape == (0, 128)
+    wq, sw = quest.quest_quantize_mx(w, 4)
+    wx, sx = quest.quest_quantize_mx(w, 8)
     r = quest.quest_linear_fwd_mx(x, w, 8)
-    assert r["y"].shape == (0, 16)
-    assert quest.quest_linear_fwd_mx(w, x, 8)["y"].shape == (16, 0)
+    assert r["y"].shape == (0, 16) and torch.equal(r["wq"], wq) and torch.equal(r["sw"], sw)
+    r = quest.quest_linear_fwd_mx(w, x, 8)
+    assert r["y"].shape == (16, 0) and torch.equal(r["xq"], wx) and torch.equal(r["sx"], sx)
+    assert quest.quest_gemm_mx(wx, sx, 8, r["wq"], r["sw"], 128).shape == (16, 0)
 
 
 def test_refusals():
