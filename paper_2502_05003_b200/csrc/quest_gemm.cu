@@ -1056,6 +1056,10 @@ int make_operand_map(CUtensorMap *tm, const int8_t *base, int64_t rows, int64_t 
     return make_map(tm, {base, K, rows, K, BK, box_rows});
 }
 
+bool tile_stores(const void *y, int64_t N, int64_t ldy, size_t esz) {
+    return reinterpret_cast<uintptr_t>(y) % 16 == 0 && (size_t)ldy * esz % 16 == 0 && (size_t)N * esz % 16 == 0;
+}
+
 int make_output_map(CUtensorMap *tm, void *base, int64_t rows, int64_t row_bytes, int64_t pitch_bytes) {
     return make_map(tm, {base, row_bytes, rows, pitch_bytes, 128, 32, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_128B,
                          CU_TENSOR_MAP_L2_PROMOTION_NONE});
@@ -1175,9 +1179,8 @@ int launch_gemm(const int8_t *a8, const int8_t *b8, const int32_t *rs_a, const i
     s = make_operand_map(&tmB, b8, N, K, narrow ? 64 : 128);
     if (s) return s;
     const bool corr = (bits_x == 8) || (bits_w == 8);
-    // y through TMA tile stores when its base and row pitch allow it (16-byte multiples)
     const size_t esz = y_dtype == QUEST_F32 ? 4 : 2;
-    const bool yt = y && (reinterpret_cast<uintptr_t>(y) % 16 == 0) && ((size_t)ldy * esz % 16 == 0);
+    const bool yt = y && tile_stores(y, N, ldy, esz);
     CUtensorMap tmY = tmA;                               // placeholder when unused
     if (yt) {
         s = make_output_map(&tmY, y, M, (int64_t)N * (int64_t)esz, (int64_t)ldy * (int64_t)esz);
@@ -1317,7 +1320,7 @@ int launch_gemm_e2m1(const uint8_t *xq, const uint8_t *wq, const float *sx, cons
     s = make_operand_map(&tmB, reinterpret_cast<const int8_t *>(wq), N, K / 2, narrow ? 64 : 128);
     if (s) return s;
     const size_t esz = y_dtype == QUEST_F32 ? 4 : 2;
-    const bool yt = y && (reinterpret_cast<uintptr_t>(y) % 16 == 0) && ((size_t)ldy * esz % 16 == 0);
+    const bool yt = y && tile_stores(y, N, ldy, esz);
     CUtensorMap tmY = tmA;
     if (yt) {
         s = make_output_map(&tmY, y, M, (int64_t)N * (int64_t)esz, (int64_t)ldy * (int64_t)esz);
@@ -1343,7 +1346,7 @@ int launch_gemm_bf16_scaled(const void *a, const void *b, const float *sw, int64
     s = make_operand_map(&tmB, reinterpret_cast<const int8_t *>(b), N, 2 * K, narrow ? 64 : 128);
     if (s) return s;
     const size_t esz = y_dtype == QUEST_F32 ? 4 : 2;
-    const bool yt = (reinterpret_cast<uintptr_t>(y) % 16 == 0) && ((size_t)ldy * esz % 16 == 0);
+    const bool yt = tile_stores(y, N, ldy, esz);
     CUtensorMap tmY = tmA;
     if (yt) {
         s = make_output_map(&tmY, y, M, (int64_t)N * (int64_t)esz, (int64_t)ldy * (int64_t)esz);

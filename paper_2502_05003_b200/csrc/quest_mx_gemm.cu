@@ -410,8 +410,7 @@ int launch_mx_gemm(const uint8_t *xq, const uint8_t *sx, int bits_x, const uint8
     };
     if ((s = scale_map(&tm[2], sx, M, 1)) || (s = scale_map(&tm[3], sw, N, bn / 128))) return s;
     const size_t esz = y_dtype == QUEST_F32 ? 4 : 2;
-    // tile stores write whole 16-byte pieces: a row of y has to end on one, or what stands behind it would be overwritten
-    const bool yt = reinterpret_cast<uintptr_t>(y) % 16 == 0 && (size_t)ldy * esz % 16 == 0 && (size_t)N * esz % 16 == 0;
+    const bool yt = tile_stores(y, N, ldy, esz);
     tm[4] = tm[0];
     if (yt && (s = make_output_map(&tm[4], y, M, N * (int64_t)esz, ldy * (int64_t)esz))) return s;
     if (x4) {

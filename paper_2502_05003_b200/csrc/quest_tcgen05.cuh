@@ -170,6 +170,9 @@ struct MapSpec {
 int make_map(CUtensorMap *tm, const MapSpec &spec);
 // int8 matrix [rows x K], K contiguous; box = 128 bytes of K x box_rows rows, 128-byte swizzle.
 int make_operand_map(CUtensorMap *tm, const int8_t *base, int64_t rows, int64_t K, int box_rows);
+// Whether y leaves by tile stores (make_output_map): base, pitch and the end of a row on 16-byte boundaries.  Tile stores write whole 16-byte pieces: of a
+// row that ends inside one they would overwrite what stands behind it.
+bool tile_stores(const void *y, int64_t N, int64_t ldy, size_t esz);
 // y viewed as bytes: [rows x row_bytes], row pitch pitch_bytes; box = 128 bytes x 32 rows, 128-byte swizzle.
 int make_output_map(CUtensorMap *tm, void *base, int64_t rows, int64_t row_bytes, int64_t pitch_bytes);
 
