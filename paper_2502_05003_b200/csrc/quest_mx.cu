@@ -21,6 +21,10 @@ struct MxQuantArgs {
 
 // A thread owns one block: 64 (bfloat16) or 128 bytes in, 16 or 32 bytes of codes and one scale byte out, nothing is
 // exchanged.  A CTA takes whole rows of whole tiles, so that the scale bytes that fill up a tile are written too (zero).
+// Bound by memory: 16384 x 4096 bfloat16 to 8 bits 32.8 us (6.2 TB/s), to 4 bits 29.3; rotated 37 and 35, where the sums,
+// conversions and maxima of a block (344 instructions) take 61 % of the issue slots between the waits for loads.  Tried without
+// gain: blocks requested one ahead (two, four, eight to a thread: 34.5 .. 36.8), more threads to an SM (41 .. 47, registers),
+// maxima of three at once and 1 / sqrt(32) folded into the scale (35.2).
 template <bool F32, bool ROTATE>
 __global__ void __launch_bounds__(256)
 mx_quantize_kernel(const __grid_constant__ MxQuantArgs a) {
@@ -61,7 +65,8 @@ struct MxDequantArgs {
     uint32_t magic;                 // ceil(2^32 / (cols / 32)); 0 for rows of one block
 };
 
-// A thread reads one block and its scale byte and writes 64 or 128 bytes.
+// A thread reads one block and its scale byte and writes 64 or 128 bytes.  Bound by the writes: 16384 x 4096 from 8 bits to
+// bfloat16 34 us (5.9 TB/s).
 template <bool F32>
 __global__ void __launch_bounds__(256)
 mx_dequantize_kernel(const __grid_constant__ MxDequantArgs a) {

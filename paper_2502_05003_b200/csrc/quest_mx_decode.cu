@@ -13,6 +13,10 @@
 // row takes elements 8 t .. 8 t + 7 of a block.  The warps' partial sums meet in shared memory.
 // FUSED (mx_fuses_quantizer): every CTA quantizes x while the first copies of w are under way, four
 // threads to a block, and leaves operands and scale bytes in shared memory.  One launch, and the host pays for one.
+//
+// Device time back to back, weights out of L2: 1 x 2048 x 2048 4.2 us fused, 3.0 from codes (the floor of 2.3 MB is 0.35: launch,
+// one round trip to memory, conversions and sums); 24 x 5504 x 2048 7.1 from codes, where conversions, products and scaling fill
+// 55 % of the issue slots.  (bfloat16 operands unpacked with shifts and masks, every CTA quantizing all of x: 7.4 and 17.2 us.)
 #include <algorithm>
 
 #include "quest_mx.cuh"

@@ -133,7 +133,8 @@ struct NormArgs {
 constexpr int row_threads(int vpt) { return vpt <= 1 ? 256 : vpt <= 4 || vpt == 16 ? 1024 : 512; }
 
 // VPT chunks to a thread; a row belongs to a warp (ROW_WARP, four rows to a CTA) or to the CTA.  MX: 0, or the bits of the
-// output: the 32 / V neighbouring lanes that hold a block agree on its scale.
+// output: the 32 / V neighbouring lanes that hold a block agree on its scale.  8192 x 2048 with residual: bfloat16 22.1 us (6.1
+// TB/s), 8-bit MX out 22.9, rotated 27 (there the ALU pipe is busy two thirds of the time); binary32 41.5 (6.5 TB/s).
 template <bool F32, bool VEC, int VPT, bool ROW_WARP, int MX>
 __global__ void __launch_bounds__(ROW_WARP ? 128 : row_threads(VPT))
 rmsnorm_kernel(const __grid_constant__ NormArgs a) {

@@ -8,6 +8,9 @@
     python -m paper_2502_05003_b200.profile_case quantize-wide       # quest_quantize alone, 8192 x 4096, one rotation block per row
     python -m paper_2502_05003_b200.profile_case mlp                 # quest_mlp_fwd, 4096 tokens, H = 2048, I = 5504
     python -m paper_2502_05003_b200.profile_case backward [calls]    # quest_linear_bwd on the config-2 layer
+    python -m paper_2502_05003_b200.profile_case mx [calls]          # quest_linear_fwd_mx, 8192 x 4096 x 4096, 4- then 8-bit activations
+    python -m paper_2502_05003_b200.profile_case mx-decode [calls]   # the same with laid-out weights, 24 x 5504 x 2048
+    python -m paper_2502_05003_b200.profile_case norm [calls]        # quest_rmsnorm_fwd (bfloat16, then 8-bit MX out) and _bwd, 8192 x 2048
 
 Inputs are random (the counters of these kernels do not depend on the values); every case cycles over buffer
 sets or tensors larger than L2 so that DRAM counters mean something, checks the device status word and prints
@@ -103,6 +106,33 @@ def backward(calls: int = 4) -> None:
         quest.quest_linear_bwd(dy, fwd, 4, 128, K, out_dtype=torch.bfloat16)
 
 
+def mx(calls: int = 2) -> None:
+    M, N, K = 8192, 4096, 4096
+    x = torch.randn(M, K, device="cuda").bfloat16()
+    wq, sw = quest.quest_quantize_mx((torch.randn(N, K, device="cuda") * 0.02).bfloat16(), 4, 32)
+    for bits in (4, 8):
+        for _ in range(calls):
+            quest.quest_linear_fwd_mx(x, None, bits, 32, w_cached={"wq": wq, "sw": sw})
+
+
+def mx_decode(calls: int = 1) -> None:
+    """40 layers, 230 MB of weights: none of them is in L2 when its turn comes."""
+    x = torch.randn(24, 2048, device="cuda").bfloat16()
+    layers = [quest.quest_quantize_mx((torch.randn(5504, 2048, device="cuda") * 0.02).bfloat16(), 4, 32) for _ in range(40)]
+    for _ in range(calls):
+        for wq, sw in layers:
+            quest.quest_linear_fwd_mx(x, None, 8, 32, w_cached={"wq": wq, "sw": sw}, want_codes=False)
+
+
+def norm(calls: int = 2) -> None:
+    x, res, dy = (torch.randn(8192, 2048, device="cuda").bfloat16() for _ in range(3))
+    weight = torch.ones(2048, device="cuda").bfloat16()
+    for _ in range(calls):
+        r = quest.quest_rmsnorm_fwd(x, weight, 1e-5, res)
+        quest.quest_rmsnorm_fwd(x, weight, 1e-5, res, mx_bits=8)
+        quest.quest_rmsnorm_bwd(dy, r["h"], weight, r["rstd"], x)
+
+
 def main() -> None:
     if not torch.cuda.is_available():
         raise SystemExit("profile_case: needs a GPU")
@@ -124,6 +154,12 @@ def main() -> None:
         mlp()
     elif case == "backward":
         backward(n or 4)
+    elif case == "mx":
+        mx(n or 2)
+    elif case == "mx-decode":
+        mx_decode(n or 1)
+    elif case == "norm":
+        norm(n or 2)
     else:
         raise SystemExit(__doc__)
     torch.cuda.synchronize()

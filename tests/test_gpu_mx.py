@@ -196,6 +196,23 @@ def test_extreme_scales(M):
 
 
 @pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("M", [2, 20, 90])
+def test_products_under_every_scale(M, bits):
+    import paper_2502_05003_b200 as quest
+    # scales that meet at 2^-8 .. 2^8 together, from both ends of their range; scale 255 is left out
+    rng = np.random.default_rng(27)
+    for sw in (0, 1, 2, 60, 127, 200, 253, 254):
+        xc = rng.integers(0, 16 if bits == 4 else 256, (M, 256)).astype(np.uint8)
+        xc[(xc & 127) == 127] = 0                              # E4M3 has two codes for NaN
+        wc, ws = rng.integers(0, 16, (40, 256)).astype(np.uint8), np.full((40, 8), sw, np.uint8)
+        xs = np.clip(254 - sw + rng.integers(-8, 9, (M, 8)), 0, 254).astype(np.uint8)
+        t = [torch.from_numpy(a).cuda() for a in (mx.pack(xc, bits), mx.tile(xs), mx.pack(wc, 4), mx.tile(ws))]
+        y = quest.quest_gemm_mx(t[0], t[1], bits, t[2], t[3], 256, F32)
+        check_product(y, mx.values(xc, xs, bits), mx.values(wc, ws, 4))
+    status()
+
+
+@pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("g", [1, 32])
 @pytest.mark.parametrize("M,N,K", [(8, 8, 128), (64, 40, 256), (264, 520, 384), (1000, 72, 1024), (48, 1032, 2048)])
 def test_gradients(M, N, K, g, bits):
