@@ -54,7 +54,7 @@ mx_quantize_kernel(const __grid_constant__ MxQuantArgs a) {
                 store_words<8>(t.codes + row * a.cols + block * MX_BLOCK, w);
             }
         }
-        t.scales[mx_scale_at(row, block, a.tiles)] = (uint8_t)s;
+        t.scales[mx_scale_at((int)row, block, a.tiles)] = (uint8_t)s;
     }
 }
 
@@ -81,7 +81,7 @@ mx_dequantize_kernel(const __grid_constant__ MxDequantArgs a) {
         const int r = a.magic ? (int)__umulhi((uint32_t)i, a.magic) : i;
         const int block = i - r * per_row;
         const long long row = row0 + r, at = row * a.cols + block * MX_BLOCK;
-        const float sc = mx_scale_f32(__ldg(t.scales + mx_scale_at(row, block, a.tiles)));
+        const float sc = mx_scale_f32(__ldg(t.scales + mx_scale_at((int)row, block, a.tiles)));
         const float2 sc2 = make_float2(sc, sc);
         float2 v[16];
         if (t.bits == 4) {

@@ -52,9 +52,10 @@ int launch_mx_few_rows(const void *x, int x_dtype, int64_t ldx, const uint8_t *x
 
 #ifdef __CUDACC__
 
-// Byte of the scale of (row, block); row_tiles_pitch = tiles of a band of 128 rows, (cols + 127) / 128.
-__device__ __forceinline__ long long mx_scale_at(long long row, int block, int tiles) {
-    return ((row >> 7) * tiles + (block >> 2)) * 512 + ((row & 31) << 4) + (((row >> 5) & 3) << 2) + (block & 3);
+// Byte of the scale of (row, block); tiles = those of a band of 128 rows, (cols + 127) / 128.  Rows are at most 2^24, tiles 128: the
+// number of a tile fits 32 bits, its place does not.
+__device__ __forceinline__ long long mx_scale_at(int row, int block, int tiles) {
+    return (long long)((row >> 7) * tiles + (block >> 2)) * 512 + (((row & 31) << 4) + (((row >> 5) & 3) << 2) + (block & 3));
 }
 
 __device__ __forceinline__ float mx_max_nan(float a, float b) {          // the larger magnitude; NaN if either is

@@ -253,7 +253,7 @@ rmsnorm_kernel(const __grid_constant__ NormArgs a) {
                 }
             }
             const int block = c / LANES;
-            if (lane % LANES == 0 && block < 4 * a.tiles) a.sy[mx_scale_at(row, block, a.tiles)] = (uint8_t)s;
+            if (lane % LANES == 0 && block < 4 * a.tiles) a.sy[mx_scale_at((int)row, block, a.tiles)] = (uint8_t)s;
         }
     }
 }
@@ -414,24 +414,30 @@ rmsnorm_bwd_kernel(const __grid_constant__ NormBwdArgs a) {
     }
 }
 
-// dw[c] = sum of `parts` rows of binary32 in a fixed order: 16 columns to a CTA, 64 groups of 16 threads take the parts in turn.
-__global__ void __launch_bounds__(1024)
+// dw[c] = sum of `parts` rows of binary32 in a fixed order: 16 columns to a CTA, SLOTS groups of 16 threads take the parts in turn.
+template <int SLOTS>
+__global__ void __launch_bounds__(16 * SLOTS)
 column_sum_kernel(const float *__restrict__ in, int parts, int cols, float *__restrict__ out) {
-    __shared__ float s[16][65];
+    __shared__ float s[16][SLOTS + 1];
     pdl_launch_dependents();
     pdl_wait();
     const int c = blockIdx.x * 16 + (threadIdx.x & 15), slot = threadIdx.x >> 4;
     float v = 0.0f;
     if (c < cols) {
 #pragma unroll 8
-        for (int p = slot; p < parts; p += 64) v += __ldg(in + (long long)p * cols + c);
+        for (int p = slot; p < parts; p += SLOTS) v += __ldg(in + (long long)p * cols + c);
     }
     s[threadIdx.x & 15][slot] = v;
     __syncthreads();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, o = blockIdx.x * 16 + warp;
-    if (warp >= 16) return;
-    v = warp_sum(s[warp][lane] + s[warp][lane + 32]);
-    if (lane == 0 && o < cols) out[o] = v;
+    const int lane = threadIdx.x & 31;
+    for (int i = threadIdx.x >> 5; i < 16; i += SLOTS / 2) {
+        v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < (SLOTS + 31) / 32; ++k)
+            if (lane + 32 * k < SLOTS) v += s[i][lane + 32 * k];
+        v = warp_sum(v);
+        if (lane == 0 && blockIdx.x * 16 + i < cols) out[blockIdx.x * 16 + i] = v;
+    }
 }
 
 bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -563,8 +569,11 @@ int quest_rmsnorm_bwd(const void *dy, const void *h, const void *dres, int dtype
         if (e != cudaSuccess) return cuda_fail(e);
     }
     if (dw) {
-        e = launch_pdl(column_sum_kernel, dim3((unsigned)((cols + 15) / 16)), dim3(1024), 0, st, 1, static_cast<const float *>(workspace), parts,
-                       (int)cols, dw);
+        const auto sum = [&](auto kernel, int slots) {
+            return launch_pdl(kernel, dim3((unsigned)((cols + 15) / 16)), dim3((unsigned)(16 * slots)), 0, st, 1, static_cast<const float *>(workspace),
+                              parts, (int)cols, dw);
+        };
+        e = parts <= 256 ? sum(column_sum_kernel<32>, 32) : sum(column_sum_kernel<64>, 64);
         if (e != cudaSuccess) return cuda_fail(e);
     }
     return QUEST_OK;
