@@ -357,9 +357,10 @@ int quest_dequantize_mx(const uint8_t *codes, const uint8_t *scales, int64_t row
  *   y                device out [M x N], y_dtype, row stride ldy_elems
  *
  * quest_linear_fwd_mx -- the layer: x (and w unless w_is_cached is 1) quantized as quest_quantize_mx does, then the product.
- *   xq, sx           device out: codes and scales of x, for a backward pass; both may be NULL where M <= 8 and M K <= 4096:
- *                    x is then quantized inside the product and nothing but y is written
+ *   xq, sx           device out: codes and scales of x, for a backward pass; both may be NULL where M <= 8, M K <= 4096
+ *                    and N <= 7104: x is then quantized inside the product and nothing but y is written
  *   wq, sw           device out, or inputs with w_is_cached = 1 (w may be NULL then)
+ * The order of the sums over K depends on M, N, K and bits_x; equal calls give equal bits.
  * No workspace.  Errors as for quest_linear_fwd.  M = 0 or N = 0: the operand that is not empty is quantized, nothing else is done.
  */
 int quest_gemm_mx(const uint8_t *xq, const uint8_t *sx, int bits_x, const uint8_t *wq, const uint8_t *sw,

@@ -631,7 +631,7 @@ def quest_linear_fwd_mx(x: torch.Tensor, w: torch.Tensor, bits_x: int = 8, had_b
     """The microscaled layer, y = x w^T with x in ``bits_x`` bits and w in 4: returns {"y", "xq", "sx", "wq", "sw"}.
 
     ``saved`` may carry preallocated tensors under those keys; ``w_cached`` = {"wq", "sw"} holds weights that are quantized
-    already (then ``w`` may be None).  With ``want_codes`` false up to 8 rows of x (and M K up to 4096) are quantized inside the
+    already (then ``w`` may be None).  With ``want_codes`` false up to 8 rows of x (M K up to 4096, N up to 7104) are quantized inside the
     product and their codes are not stored (None); more rows need the room all the same.  ``x`` or ``w`` whose rows do not start on
     16-byte boundaries, or with another inner stride, is copied first."""
     done = _lib.binding().linear_fwd_mx(x, w, bits_x, had_block, out_dtype, y, saved, w_cached, want_codes)
@@ -669,7 +669,7 @@ def quest_linear_fwd_mx(x: torch.Tensor, w: torch.Tensor, bits_x: int = 8, had_b
             _mx_scales_of(name, "sw", out["sw"], N, K)
         _kept(name, out, "wq", (N, K // 2), torch.uint8, dev)
         _kept(name, out, "sw", (quest_mx_scales_bytes(N, K),), torch.uint8, dev)
-        if want_codes or M > 8 or M * K > 4096:
+        if want_codes or M > 8 or M * K > 4096 or N > 7104:
             _kept(name, out, "xq", (M, K * bits_x // 8), torch.uint8, dev)
             _kept(name, out, "sx", (quest_mx_scales_bytes(M, K),), torch.uint8, dev)
         else:

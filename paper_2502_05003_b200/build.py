@@ -32,6 +32,7 @@ UNITS = {
     "quest_mx.cu": ["-fmad=false"],
     "quest_mx_decode.cu": ["-fmad=false"],
     "quest_mx_gemm.cu": [],
+    "quest_mx_thin.cu": [],
     "quest_norm.cu": ["-fmad=false"],
 }
 

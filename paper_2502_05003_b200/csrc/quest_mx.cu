@@ -142,6 +142,14 @@ int check_product(const uint8_t *wq, const uint8_t *sw, int bits_x, int64_t M, i
     if (!aligned(wq, bits_x == 8 ? 32 : 16) || !aligned(sw, 16) || !aligned(y, y_dtype == QUEST_F32 ? 4 : 2)) return QUEST_ERR_ALIGN;
     return QUEST_OK;
 }
+int product_of_codes(const uint8_t *xq, const uint8_t *sx, int bits_x, const uint8_t *wq, const uint8_t *sw, int64_t M, int64_t N, int64_t K,
+                     void *y, int y_dtype, int64_t ldy, cudaStream_t st) {
+    switch (mx_product(M, N, K, bits_x)) {
+        case MxProduct::few: return launch_mx_few_rows(nullptr, 0, 0, xq, sx, bits_x, 1, wq, sw, M, N, K, y, y_dtype, ldy, st);
+        case MxProduct::thin: return launch_mx_thin(xq, sx, bits_x, wq, sw, M, N, K, y, y_dtype, ldy, st);
+        default: return launch_mx_gemm(xq, sx, bits_x, wq, sw, M, N, K, y, y_dtype, ldy, st);
+    }
+}
 
 }  // namespace
 
@@ -237,8 +245,7 @@ int quest_gemm_mx(const uint8_t *xq, const uint8_t *sx, int bits_x, const uint8_
     if ((s = check_device())) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     void *h = stage_begin(QUEST_STAGE_GEMM, st);
-    s = M <= MX_FEW_ROWS ? launch_mx_few_rows(nullptr, 0, 0, xq, sx, bits_x, 1, wq, sw, M, N, K, y, y_dtype, ldy_elems, st)
-                         : launch_mx_gemm(xq, sx, bits_x, wq, sw, M, N, K, y, y_dtype, ldy_elems, st);
+    s = product_of_codes(xq, sx, bits_x, wq, sw, M, N, K, y, y_dtype, ldy_elems, st);
     stage_end(h);
     return s;
 }
@@ -253,9 +260,9 @@ int quest_linear_fwd_mx(const void *x, int x_dtype, int64_t ldx, const void *w, 
     if (!w_is_cached && (s = check_rows(w, w_dtype, N, K, ldw))) return s;
     if (!mx_had_ok(had_block)) return QUEST_ERR_HAD_BLOCK;
     // an empty product still quantizes the operand that there is
-    const bool few = M <= MX_FEW_ROWS, keep = M > 0 && (xq || sx), quantize_w = N > 0 && !w_is_cached;
+    const bool keep = M > 0 && (xq || sx), quantize_w = N > 0 && !w_is_cached;
     if (quantize_w && (!wq || !sw)) return QUEST_ERR_NULL;
-    if ((keep || (M > 0 && N > 0 && !mx_fuses_quantizer(M, K))) && (!xq || !sx)) return QUEST_ERR_NULL;
+    if ((keep || (M > 0 && N > 0 && !mx_fuses_quantizer(M, N, K))) && (!xq || !sx)) return QUEST_ERR_NULL;
     if ((keep && (!aligned(xq, 16) || !aligned(sx, 16))) || (quantize_w && !aligned(wq, 16))) return QUEST_ERR_ALIGN;
     if ((M == 0 || N == 0) && !keep && !quantize_w) return QUEST_OK;
     if ((s = check_device())) return s;
@@ -279,8 +286,7 @@ int quest_linear_fwd_mx(const void *x, int x_dtype, int64_t ldx, const void *w, 
     }
     if (M == 0 || N == 0) return QUEST_OK;
     void *h = stage_begin(QUEST_STAGE_GEMM, st);
-    if (!few) s = launch_mx_gemm(xq, sx, bits_x, wq, sw, M, N, K, y, y_dtype, ldy_elems, st);
-    else if (keep) s = launch_mx_few_rows(nullptr, 0, 0, xq, sx, bits_x, 1, wq, sw, M, N, K, y, y_dtype, ldy_elems, st);
+    if (keep) s = product_of_codes(xq, sx, bits_x, wq, sw, M, N, K, y, y_dtype, ldy_elems, st);
     else s = launch_mx_few_rows(x, x_dtype, ldx, nullptr, nullptr, bits_x, had_block, wq, sw, M, N, K, y, y_dtype, ldy_elems, st);
     stage_end(h);
     return s;

@@ -41,14 +41,32 @@ int launch_mx_dequantize(const MxDequantJob *jobs, int njobs, int dtype, int64_t
 // y = x w^T over blocks: x 4 or 8 bits, w 4 bits (quest_mx_gemm.cu).
 int launch_mx_gemm(const uint8_t *xq, const uint8_t *sx, int bits_x, const uint8_t *wq, const uint8_t *sw, int64_t M, int64_t N,
                    int64_t K, void *y, int y_dtype, int64_t ldy, cudaStream_t st);
+// The same with the sides of the tensor cores' tiles exchanged and, where that fills the chip, K split (quest_mx_thin.cu).
+int launch_mx_thin(const uint8_t *xq, const uint8_t *sx, int bits_x, const uint8_t *wq, const uint8_t *sw, int64_t M, int64_t N, int64_t K,
+                   void *y, int y_dtype, int64_t ldy, cudaStream_t st);
 // The product for a few rows of x (quest_mx_decode.cu), which are quantized on the way (x) or are given as codes (xq, sx).
-constexpr int MX_FEW_ROWS = 32;
-// Whether that product quantizes x itself: up to eight rows of which a thread of the CTA takes one quarter of a block.  More, and
-// a launch of the quantizer in front costs less (8 x 2048 x 2048: 7.7 us against 4.9; 1 x 2048 x 2048: 4.2 against 4.4).
-inline bool mx_fuses_quantizer(int64_t M, int64_t K) { return M <= 8 && M * K <= 4096; }
 int launch_mx_few_rows(const void *x, int x_dtype, int64_t ldx, const uint8_t *xq, const uint8_t *sx, int bits_x, int had_block,
                        const uint8_t *wq, const uint8_t *sw, int64_t M, int64_t N, int64_t K, void *y, int y_dtype, int64_t ldy,
                        cudaStream_t st);
+
+// Which of the three.  Up to 32 rows go without tensor memory while w is small: its rows fill one round of CTAs, and K is short enough
+// for one CTA to walk.  Time of the exchanged tiles over that kernel's, 8 and 4 bits: 8 x 4096 x 4096 1.10 / 0.98, 8 x 8192 x 2048
+// 0.77 / 0.60, 8 x 2048 x 8192 0.75 / 0.63, 24 x 2048 x 2048 1.16 / 1.06, 24 x 5504 x 2048 0.78 / 0.62, 32 x 32000 x 4096 0.21 / 0.25.
+// Above, the exchanged tiles against pairs of CTAs on 256 rows of x: 64 x 4096 x 4096 0.71 / 0.87, 128 x 2048 x 8192 0.52 / 0.67;
+// more than 128 rows 0.5 .. 1.04 where w fills a side of 128 and the tiles take half of the SMs (K is split) or one
+// short round, else 0.8 .. 1.3.
+enum class MxProduct { few, thin, wide };
+constexpr int64_t MX_SMS = 148;
+inline MxProduct mx_product(int64_t M, int64_t N, int64_t K, int bits_x) {
+    const int64_t per_sm = M <= 8 ? 48 : M <= 16 ? 32 : 24;
+    if (M <= 32 && N <= per_sm * MX_SMS && (M < 8 ? 8 : M) * K < 65536) return MxProduct::few;
+    const int64_t tiles = (N + 127) / 128 * ((M + 127) / 128);
+    const bool fits = N >= 128 && (2 * tiles <= MX_SMS || (tiles <= MX_SMS && K <= (bits_x == 4 ? 2048 : 1024)));
+    return M <= 128 || fits ? MxProduct::thin : MxProduct::wide;
+}
+// Whether the product of few rows quantizes x itself: up to eight of which a thread of the CTA takes one quarter of a block.  More, and
+// a launch of the quantizer in front costs less (8 x 2048 x 2048: 7.7 us against 4.9; 1 x 2048 x 2048: 4.2 against 4.4).
+inline bool mx_fuses_quantizer(int64_t M, int64_t N, int64_t K) { return M <= 8 && M * K <= 4096 && N <= 48 * MX_SMS; }
 
 #ifdef __CUDACC__
 

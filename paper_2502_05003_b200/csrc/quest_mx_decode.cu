@@ -1,8 +1,8 @@
-// The microscaled product for a few rows of x (a decoding step): y[m][n] = sum_k x[m][k] w[n][k], up to 32 rows m.
+// The microscaled product for a few rows of x and a small w (mx_product): y[m][n] = sum_k x[m][k] w[n][k], up to 32 rows m.
 //
 // Bound by reading w (4.25 bits an element) and, beside that, by the instructions that turn codes into operands, so it runs on
-// mma.sync m16n8k16 with the rows of w as the 16-wide side: a tcgen05 tile would be empty but for these rows, and 128 rows of w
-// a CTA would leave most SMs without one.  Codes become binary16 operands with the hardware conversions, two elements an
+// mma.sync m16n8k16 with the rows of w as the 16-wide side: 128 rows of w a CTA, as the tcgen05 products take, would leave most SMs
+// without one or cost sums over a cluster.  Codes become binary16 operands with the hardware conversions, two elements an
 // instruction and exactly (E2M1 has 2 and E4M3 4 significant bits); their scales, which may pass binary16's range, stay out:
 // a block of 32 is two products from zero, and its sums join the accumulators times 2^(sw + sx) in binary32:
 //     acc[n][m] += (2^sw[n] 2^sx[m]) sum_32 qw[n] qx[m]
@@ -15,8 +15,9 @@
 // threads to a block, and leaves operands and scale bytes in shared memory.  One launch, and the host pays for one.
 //
 // Device time back to back, weights out of L2: 1 x 2048 x 2048 4.2 us fused, 3.0 from codes (the floor of 2.3 MB is 0.35: launch,
-// one round trip to memory, conversions and sums); 24 x 5504 x 2048 7.1 from codes, where conversions, products and scaling fill
-// 55 % of the issue slots.  (bfloat16 operands unpacked with shifts and masks, every CTA quantizing all of x: 7.4 and 17.2 us.)
+// one round trip to memory, conversions and sums); 24 x 2048 x 2048 4.7 from codes, where conversions, products and scaling fill 37 % of
+// the issue slots.  (bfloat16 operands unpacked with shifts and masks, every CTA quantizing all of x: 7.4 us for 24 x 5504 x 2048 from
+// codes, 17.2 from values, against 7.1 for this form.)
 #include <algorithm>
 
 #include "quest_mx.cuh"
@@ -297,7 +298,9 @@ cudaError_t launch_shape(const FewArgs &a, cudaStream_t st) {
 }
 template <int XB, int TT, bool FUSED>
 cudaError_t launch_rows(const FewArgs &a, int rt, cudaStream_t st) {
-    return rt == 1 ? launch_shape<XB, TT, 1, FUSED>(a, st) : rt == 2 ? launch_shape<XB, TT, 2, FUSED>(a, st) : launch_shape<XB, TT, 3, FUSED>(a, st);
+    if (rt == 1) return launch_shape<XB, TT, 1, FUSED>(a, st);
+    if constexpr (TT == 1) return launch_shape<XB, TT, 3, FUSED>(a, st);
+    else return launch_shape<XB, TT, 2, FUSED>(a, st);
 }
 template <int XB>
 cudaError_t launch_tokens(const FewArgs &a, int rt, cudaStream_t st) {
@@ -314,9 +317,9 @@ int launch_mx_few_rows(const void *x, int x_dtype, int64_t ldx, const uint8_t *x
     const FewArgs a = {x, xq, sx, (long long)ldx, wq, sw, (int)M, (int)N, (int)K, (int)((K + 127) / 128), y, (long long)ldy,
                        x_dtype == QUEST_F32, had_block == 32, y_dtype == QUEST_F32};
     // rows of w a CTA: as few as one round of CTAs allows, for up to eight rows of x two 16-row CTAs to an SM (24 x 5504 x 2048 from
-    // codes: 48 rows a CTA 7.8 us, 32 10.4, 16 11.3; 8 x 4096 x 4096: 16 rows 5.6, 48 6.5)
+    // codes: 48 rows a CTA 7.8 us, 32 10.4, 16 11.3; 8 x 4096 x 4096: 16 rows 5.6, 48 6.5).  Longer w does not come here (mx_product)
     const int64_t sms = num_sms();
-    const int rt = N <= 16 * sms * (M <= 8 ? 2 : 1) ? 1 : N <= 32 * sms ? 2 : 3;
+    const int rt = M <= 8 ? (N <= 32 * sms ? 1 : 3) : N <= 16 * sms ? 1 : 2;
     const cudaError_t e = bits_x == 4 ? launch_tokens<4>(a, rt, st) : launch_tokens<8>(a, rt, st);
     return e == cudaSuccess ? QUEST_OK : cuda_fail(e);
 }

@@ -21,8 +21,7 @@
 // has left for registers.  Few tiles: 768 x 2048 x 5504 takes 12 us, 43 k-blocks at 0.17 us and 4.5 us of launch, first loads and last epilogue.
 #include <algorithm>
 
-#include "quest_mx.cuh"
-#include "quest_tcgen05.cuh"
+#include "quest_mx_tcgen05.cuh"
 
 namespace quest {
 namespace {
@@ -42,14 +41,6 @@ struct MxGemmParams {
     int *status;
 };
 
-// Instruction descriptor, block-scaled kinds: element types of A and B, UE8M0 scales, M, N; the scale byte of a
-// 32-bit word that an instruction starts from (sf) goes into bits 4 (B) and 29 (A).
-template <int XB>
-__host__ __device__ constexpr uint32_t make_idesc(int m, int n) {
-    // kind::mxf4: E2M1 is type 1.  kind::mxf8f6f4: E4M3 is type 0, E2M1 type 5.
-    return ((XB == 4 ? 1u : 0u) << 7) | ((XB == 4 ? 1u : 5u) << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) |
-           ((uint32_t)(m >> 7) << 27);
-}
 template <int XB>
 __device__ __forceinline__ void umma_mx_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate,
                                              uint32_t sfa_tmem, uint32_t sfb_tmem) {
@@ -72,10 +63,6 @@ __device__ __forceinline__ void umma_mx_pair(uint32_t d_tmem, uint64_t a_desc, u
 // four lane quarters.
 __device__ __forceinline__ void scales_to_tmem_pair(uint32_t taddr, uint64_t desc) {
     asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-}
-// Descriptor of such a tile: no swizzle, groups of eight 16-byte rows 128 bytes apart.
-__device__ __forceinline__ uint64_t make_scale_desc(uint32_t smem_addr) {
-    return (uint64_t)((smem_addr & 0x3FFFF) >> 4) | (uint64_t)1 << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
 }
 
 // Shared memory from a 1024-byte-aligned base: output staging, barriers, then the ring.
@@ -217,7 +204,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         __syncwarp();
     } else if (warp == 1) {
         if (leader && elect_one()) {
-            constexpr uint32_t idesc = make_idesc<XB>(TILE_M, BN);
+            constexpr uint32_t idesc = mx_idesc(XB == 4 ? 1 : 0, XB == 4 ? 1 : 5, TILE_M, BN);
             const int num_whole = p.K / KB;
             int stage = 0, t = 0, slot = 0;
             uint32_t phase = 0;
@@ -405,19 +392,12 @@ int launch_mx_gemm(const uint8_t *xq, const uint8_t *sx, int bits_x, const uint8
     // rounds, 0.92 .. 1.02 at three to two, 0.93 .. 1.07 at five to three, above that 1.0 .. 1.23 (70 shapes in both widths: within
     // 0.1 % of the better choice of each on average)
     const bool narrow = 2 * rounds128 <= 3 * rounds256;
-    const int64_t tiles = (K + 127) / 128;
     const int groups = x4 ? 2 : 1, bn = narrow ? 128 : 256;
     CUtensorMap tm[5];
     int s;
-    if ((s = make_map(&tm[0], {xq, K * bits_x / 8, M, K * bits_x / 8, BK, BM}))) return s;
-    if (x4) s = make_map(&tm[1], {wq, K / 2, N, K / 2, BK, bn / 2});
-    else s = make_map(&tm[1], {wq, K, N, K / 2, BK, bn / 2, CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B});
-    if (s) return s;
-    const auto scale_map = [&](CUtensorMap *m, const uint8_t *scales, int64_t rows, int box_bands) {
-        return make_map(m, {scales, 128 * tiles, (rows + 127) / 128, 512 * tiles, 128 * groups, box_bands, CU_TENSOR_MAP_DATA_TYPE_UINT32,
-                            CU_TENSOR_MAP_SWIZZLE_NONE});
-    };
-    if ((s = scale_map(&tm[2], sx, M, 1)) || (s = scale_map(&tm[3], sw, N, bn / 128))) return s;
+    if ((s = make_map(&tm[0], {xq, K * bits_x / 8, M, K * bits_x / 8, BK, BM})) || (s = mx_weight_map(&tm[1], wq, N, K, !x4, bn / 2)) ||
+        (s = mx_scale_map(&tm[2], sx, M, K, groups, 1)) || (s = mx_scale_map(&tm[3], sw, N, K, groups, bn / 128)))
+        return s;
     const size_t esz = y_dtype == QUEST_F32 ? 4 : 2;
     const bool yt = tile_stores(y, N, ldy, esz);
     tm[4] = tm[0];
