@@ -263,9 +263,17 @@ mx_thin_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ 
             }
         }
     }
+    // tensor memory goes back before anybody waits for the cluster: another kernel's CTA may need it to let one of the cluster start
+    tc_fence_before();
+    __syncwarp();
+    if (splits > 1) cluster_arrive();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(L::TMEM_COLS) : "memory");
+    }
     if (splits > 1) {
         __syncwarp();
-        cluster_arrive();
         cluster_wait();
         if (warp >= 2) {
             const int own = (live + splits - 1) / splits, first = split * own, last = min(first + own, live);
@@ -292,12 +300,6 @@ mx_thin_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ 
         __syncwarp();
         cluster_arrive();                        // nobody leaves while others read its sums
         cluster_wait();
-    }
-    tc_fence_before();
-    __syncthreads();
-    if (warp == 1) {
-        tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(L::TMEM_COLS) : "memory");
     }
 }
 
