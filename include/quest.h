@@ -398,6 +398,7 @@ size_t quest_bwd_mx_workspace_bytes(int64_t M, int64_t N, int64_t K);
  *   y, y_dtype       device out, dense; NULL if mx_bits is not 0
  *   mx_bits          0: y.  4 or 8: yq, sy as quest_quantize_mx(y) in that many bits with had_block (1 or 32) writes them; then
  *                    cols is a multiple of 32 and every row of x, residual and h starts on a 16-byte boundary, and yq does
+ *   h (or y, where there is no MX output) may be the memory of x or residual, where that is dense and of its type.
  *   1 <= cols <= 16384, 0 <= rows <= 2^24.  Without MX output no alignment beyond that of an element is asked for (rows on
  *   16-byte boundaries are faster).
  *
@@ -405,7 +406,8 @@ size_t quest_bwd_mx_workspace_bytes(int64_t M, int64_t N, int64_t K);
  *     dx = dres + rstd (g - n mean(g n)),   dw = sum over rows of dy n
  *   dx is the gradient of x and of the residual alike.  dy, h, dres (may be NULL): dtype, row strides lddy, ldh, lddr;
  *   rstd: what the forward call wrote; dx device out, dense, dtype; dw device out [cols] binary32, summed in a fixed order; either
- *   may be NULL.  workspace: quest_rmsnorm_bwd_workspace_bytes(rows, cols) bytes, 256-byte aligned.
+ *   may be NULL; dx may be the memory of dy, h or dres, where that is dense.
+ *   workspace: quest_rmsnorm_bwd_workspace_bytes(rows, cols) bytes, 256-byte aligned.
  */
 int quest_rmsnorm_fwd(const void *x, const void *residual, int dtype, int64_t ldx, int64_t ldr, const void *weight, int w_dtype,
                       int64_t rows, int64_t cols, float eps, void *h, float *rstd, void *y, int y_dtype,

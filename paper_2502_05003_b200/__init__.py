@@ -630,7 +630,7 @@ def quest_linear_fwd_mx(x: torch.Tensor, w: torch.Tensor, bits_x: int = 8, had_b
                         y: torch.Tensor = None, saved: dict = None, w_cached: dict = None, want_codes: bool = True) -> dict:
     """The microscaled layer, y = x w^T with x in ``bits_x`` bits and w in 4: returns {"y", "xq", "sx", "wq", "sw"}.
 
-    ``saved`` may carry preallocated tensors under those keys; ``w_cached`` = {"wq", "sw"} holds weights that are quantized
+    ``saved`` may carry preallocated tensors for the codes and scales; ``w_cached`` = {"wq", "sw"} holds weights that are quantized
     already (then ``w`` may be None).  With ``want_codes`` false up to 8 rows of x (M K up to 4096, N up to 7104) are quantized inside the
     product and their codes are not stored (None); more rows need the room all the same.  ``x`` or ``w`` whose rows do not start on
     16-byte boundaries, or with another inner stride, is copied first."""
@@ -739,7 +739,7 @@ def quest_rmsnorm_fwd(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, 
                       mx_bits: int = None, had_block: int = 1, out: dict = None, want_rstd: bool = True) -> dict:
     """h = x + residual, y = h (mean(h^2) + eps)^(-1/2) weight for every row.  Returns {"h" (None without a residual),
     "rstd" [rows] or None, and "y" or, with ``mx_bits`` 4 or 8, "yq", "sy": the codes and scales that ``quest_gemm_mx``
-    takes}.  ``out`` may hold preallocated tensors under those keys."""
+    takes}.  ``out`` may hold preallocated tensors under those keys; "h" or "y" may be ``x`` or ``residual`` itself."""
     done = _lib.binding().rmsnorm_fwd(x, weight, eps, residual, out_dtype, mx_bits, had_block, out, want_rstd)
     if done is not None:
         return _result(done)
@@ -787,7 +787,7 @@ def quest_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, r
                       out: dict = None, want_dx: bool = True, want_dw: bool = True, workspace: torch.Tensor = None) -> dict:
     """Gradient of ``quest_rmsnorm_fwd``: ``h`` is what was normalised (the forward call's "h", or x without a residual),
     ``dres`` the gradient that reaches h on the residual stream.  Returns {"dx": the gradient of x and of the residual, "dw":
-    float32 [cols]}; ``out`` may hold preallocated tensors under those keys."""
+    float32 [cols]}; ``out`` may hold preallocated tensors under those keys, "dx" may be ``dy``, ``h`` or ``dres`` itself."""
     done = _lib.binding().rmsnorm_bwd(dy, h, weight, rstd, dres, out, want_dx, want_dw, workspace)
     if done is not None:
         return _result(done)

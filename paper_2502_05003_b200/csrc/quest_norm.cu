@@ -18,16 +18,17 @@ template <bool F32, bool VEC>
 struct Chunk {
     static constexpr int V = VEC ? (F32 ? 4 : 8) : 1;
     uint32_t w[VEC ? 4 : 1];
-    // volatile: requested where it stands, not where the compiler would use it (a row ahead, behind a barrier)
+    // volatile: requested where it stands, not where the compiler would use it (a row ahead, behind a barrier).  Not as read-only
+    // data: an output may take an input's place
     __device__ __forceinline__ void load(const void *p, long long i) {
         const uint8_t *at = static_cast<const uint8_t *>(p) + i * (F32 ? 4 : 2);
         if constexpr (VEC) {
-            asm volatile("ld.global.nc.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(at));
+            asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(at));
         } else if constexpr (F32) {
-            asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(w[0]) : "l"(at));
+            asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(at));
         } else {
             uint16_t v;
-            asm volatile("ld.global.nc.b16 %0, [%1];" : "=h"(v) : "l"(at));
+            asm volatile("ld.global.b16 %0, [%1];" : "=h"(v) : "l"(at));
             w[0] = v;
         }
     }
