@@ -50,8 +50,9 @@ int launch_mx_few_rows(const void *x, int x_dtype, int64_t ldx, const uint8_t *x
                        cudaStream_t st);
 
 // Which of the three.  Up to 32 rows go without tensor memory while w is small: its rows fill one round of CTAs, and K is short enough
-// for one CTA to walk.  Time of the exchanged tiles over that kernel's, 8 and 4 bits: 8 x 4096 x 4096 1.10 / 0.98, 8 x 8192 x 2048
-// 0.77 / 0.60, 8 x 2048 x 8192 0.75 / 0.63, 24 x 2048 x 2048 1.16 / 1.06, 24 x 5504 x 2048 0.78 / 0.62, 32 x 32000 x 4096 0.21 / 0.25.
+// for one CTA to walk.  Time of the exchanged tiles over that kernel's, 8 and 4 bits: 8 x 2048 x 2048 1.12 / 1.02, x 4096 0.91 / 0.79,
+// x 8192 0.75 / 0.62; 8 x 4096 x 2048 1.17 / 1.06, 8 x 8192 x 2048 0.75 / 0.62; 16 x 2048 x 2048 1.15 / 0.83, x 2560 0.98 / 0.72; 24 x 2048 x
+// 1024 0.96 / 1.11, x 1536 0.92 / 1.08, x 2048 0.95 / 0.96; 32 x 2048 x 768 0.92 / 0.96; 32 x 32000 x 4096 0.21 / 0.25.
 // Above, the exchanged tiles against pairs of CTAs on 256 rows of x: 64 x 4096 x 4096 0.71 / 0.87, 128 x 2048 x 8192 0.52 / 0.67;
 // more than 128 rows 0.5 .. 1.04 where w fills a side of 128 and the tiles take half of the SMs (K is split) or one
 // short round, else 0.8 .. 1.3.
@@ -59,7 +60,7 @@ enum class MxProduct { few, thin, wide };
 constexpr int64_t MX_SMS = 148;
 inline MxProduct mx_product(int64_t M, int64_t N, int64_t K, int bits_x) {
     const int64_t per_sm = M <= 8 ? 48 : M <= 16 ? 32 : 24;
-    if (M <= 32 && N <= per_sm * MX_SMS && (M < 8 ? 8 : M) * K < 65536) return MxProduct::few;
+    if (M <= 32 && N <= per_sm * MX_SMS && (M < 8 ? 8 : M) * K <= 32768) return MxProduct::few;
     const int64_t tiles = (N + 127) / 128 * ((M + 127) / 128);
     const bool fits = N >= 128 && (2 * tiles <= MX_SMS || (tiles <= MX_SMS && K <= (bits_x == 4 ? 2048 : 1024)));
     return M <= 128 || fits ? MxProduct::thin : MxProduct::wide;

@@ -15,7 +15,7 @@
 // threads to a block, and leaves operands and scale bytes in shared memory.  One launch, and the host pays for one.
 //
 // Device time back to back, weights out of L2: 1 x 2048 x 2048 4.2 us fused, 3.0 from codes (the floor of 2.3 MB is 0.35: launch,
-// one round trip to memory, conversions and sums); 24 x 2048 x 2048 4.7 from codes, where conversions, products and scaling fill 37 % of
+// one round trip to memory, conversions and sums); 16 x 2048 x 2048 3.7 from codes, where conversions, products and scaling fill 29 % of
 // the issue slots.  (bfloat16 operands unpacked with shifts and masks, every CTA quantizing all of x: 7.4 us for 24 x 5504 x 2048 from
 // codes, 17.2 from values, against 7.1 for this form.)
 #include <algorithm>

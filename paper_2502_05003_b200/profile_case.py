@@ -9,7 +9,7 @@
     python -m paper_2502_05003_b200.profile_case mlp                 # quest_mlp_fwd, 4096 tokens, H = 2048, I = 5504
     python -m paper_2502_05003_b200.profile_case backward [calls]    # quest_linear_bwd on the config-2 layer
     python -m paper_2502_05003_b200.profile_case mx [calls]          # quest_linear_fwd_mx, 8192 x 4096 x 4096, 4- then 8-bit activations
-    python -m paper_2502_05003_b200.profile_case mx-decode [calls]   # the same with laid-out weights, 24 x 5504 x 2048, then 24 x 2048 x 2048
+    python -m paper_2502_05003_b200.profile_case mx-decode [calls]   # the same with laid-out weights, 24 x 5504 x 2048, then 16 x 2048 x 2048
     python -m paper_2502_05003_b200.profile_case norm [calls]        # quest_rmsnorm_fwd (bfloat16, then 8-bit MX out) and _bwd, 8192 x 2048
 
 Inputs are random (the counters of these kernels do not depend on the values); every case cycles over buffer
@@ -121,7 +121,7 @@ def mx_decode(calls: int = 1) -> None:
     layers = [quest.quest_quantize_mx((torch.randn(n, 2048, device="cuda") * 0.02).bfloat16(), 4, 32) for n in [5504] * 40 + [2048] * 60]
     for _ in range(calls):
         for wq, sw in layers:
-            quest.quest_linear_fwd_mx(x, None, 8, 32, w_cached={"wq": wq, "sw": sw}, want_codes=False)
+            quest.quest_linear_fwd_mx(x if wq.shape[0] == 5504 else x[:16], None, 8, 32, w_cached={"wq": wq, "sw": sw}, want_codes=False)
 
 
 def norm(calls: int = 2) -> None:
