@@ -66,7 +66,7 @@ inline MxProduct mx_product(int64_t M, int64_t N, int64_t K, int bits_x) {
     return M <= 128 || fits ? MxProduct::thin : MxProduct::wide;
 }
 // Whether the product of few rows quantizes x itself: up to eight of which a thread of the CTA takes one quarter of a block.  More, and
-// a launch of the quantizer in front costs less (8 x 2048 x 2048: 7.7 us against 4.9; 1 x 2048 x 2048: 4.2 against 4.4).
+// a launch of the quantizer in front costs less (8 x 2048 x 2048: 7.7 us against 4.9; 1 x 2048 x 2048: 3.8 against 4.2, 2 x 2048 x 2048 4.2 against 4.3).
 inline bool mx_fuses_quantizer(int64_t M, int64_t N, int64_t K) { return M <= 8 && M * K <= 4096 && N <= 48 * MX_SMS; }
 
 #ifdef __CUDACC__
