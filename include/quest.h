@@ -397,7 +397,8 @@ size_t quest_bwd_mx_workspace_bytes(int64_t M, int64_t N, int64_t K);
  *   rstd             device out [rows] binary32, or NULL
  *   y, y_dtype       device out, dense; NULL if mx_bits is not 0
  *   mx_bits          0: y.  4 or 8: yq, sy as quest_quantize_mx(y) in that many bits with had_block (1 or 32) writes them; then
- *                    cols is a multiple of 32 and every row of x, residual and h starts on a 16-byte boundary, and yq does
+ *                    cols is a multiple of 32 and every row of x, residual and h starts on a 16-byte boundary, and weight
+ *                    and yq do
  *   h (or y, where there is no MX output) may be the memory of x or residual, where that is dense and of its type.
  *   1 <= cols <= 16384, 0 <= rows <= 2^24.  Without MX output no alignment beyond that of an element is asked for (rows on
  *   16-byte boundaries are faster).

@@ -647,7 +647,7 @@ def quest_linear_fwd_mx(x: torch.Tensor, w: torch.Tensor, bits_x: int = 8, had_b
     def rows(key, t):
         if t.dim() != 2:
             raise ValueError(f"{name}: {key} must be 2-D")
-        if t.stride(1) != 1 or t.stride(0) < t.shape[1] or t.data_ptr() % 16 or t.stride(0) * t.element_size() % 16:
+        if t.stride(1) != 1 or t.data_ptr() % 16 or (t.shape[0] > 1 and (t.stride(0) < t.shape[1] or t.stride(0) * t.element_size() % 16)):
             t = t.contiguous()
         if t.data_ptr() % 16:
             t = t.clone()

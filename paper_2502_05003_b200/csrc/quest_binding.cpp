@@ -496,7 +496,7 @@ int64_t mx_scales(int64_t rows, int64_t cols) {
     return n;
 }
 bool on_16(const at::Tensor &t) {          // rows that the C ABI takes as they are
-    return reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0 && t.stride(0) * (int64_t)t.element_size() % 16 == 0;
+    return reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0 && (t.size(0) == 1 || t.stride(0) * (int64_t)t.element_size() % 16 == 0);
 }
 // The tensor under a dictionary's key with room for `bytes`, or a new one that is put there; its memory.
 void *keep(Named &d, PyObject *key, const at::Tensor &x, at::IntArrayRef shape, at::ScalarType type) {

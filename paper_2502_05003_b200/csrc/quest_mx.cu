@@ -125,7 +125,7 @@ int check_rows(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld)
     if (!x && rows != 0) return QUEST_ERR_NULL;
     if (dtype != QUEST_F32 && dtype != QUEST_BF16) return QUEST_ERR_DTYPE;
     if (!mx_rows_ok(rows) || !mx_cols_ok(cols) || ld < cols) return QUEST_ERR_SHAPE;
-    if (!aligned(x, 16) || ld * (dtype == QUEST_F32 ? 4 : 2) % 16 != 0) return QUEST_ERR_ALIGN;
+    if (!aligned(x, 16) || (rows > 1 && ld * (dtype == QUEST_F32 ? 4 : 2) % 16 != 0)) return QUEST_ERR_ALIGN;
     return QUEST_OK;
 }
 

@@ -442,6 +442,7 @@ column_sum_kernel(const float *__restrict__ in, int parts, int cols, float *__re
 }
 
 bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+bool pitch_ok(int64_t rows, int64_t bytes) { return rows == 1 || bytes % 16 == 0; }       // a lone row has no next one
 bool shape_ok(int64_t rows, int64_t cols) { return mx_rows_ok(rows) && cols >= 1 && cols <= 16384; }
 
 // Most CTAs of the backward kernel, hence rows of partial sums.
@@ -524,8 +525,8 @@ int quest_rmsnorm_fwd(const void *x, const void *residual, int dtype, int64_t ld
     if (!aligned(x, es) || !aligned(weight, ws) || (residual && (!aligned(residual, es) || !aligned(h, es))) || (rstd && !aligned(rstd, 4)) ||
         (!mx_bits && !aligned(y, ys)))
         return QUEST_ERR_ALIGN;
-    const bool vec = cols % 8 == 0 && aligned(x, 16) && ldx * es % 16 == 0 && aligned(weight, 16) &&
-                     (!residual || (aligned(residual, 16) && ldr * es % 16 == 0 && aligned(h, 16))) && (mx_bits ? aligned(yq, 16) : aligned(y, 16));
+    const bool vec = cols % 8 == 0 && aligned(x, 16) && pitch_ok(rows, ldx * es) && aligned(weight, 16) &&
+                     (!residual || (aligned(residual, 16) && pitch_ok(rows, ldr * es) && aligned(h, 16))) && (mx_bits ? aligned(yq, 16) : aligned(y, 16));
     if (mx_bits && !vec) return QUEST_ERR_ALIGN;
     const int s = check_device();
     if (s) return s;
@@ -565,7 +566,7 @@ int quest_rmsnorm_bwd(const void *dy, const void *h, const void *dres, int dtype
         const NormBwdArgs a = {dy, h, dres, weight, rstd, (long long)lddy, (long long)ldh, (long long)lddr, (long long)rows, (int)cols,
                                w_dtype == QUEST_F32, dx, dw ? static_cast<float *>(workspace) : nullptr};
         const bool vec = cols % 8 == 0 && aligned(dy, 16) && aligned(h, 16) && aligned(dres, 16) && aligned(dx, 16) && aligned(weight, 16) &&
-                         lddy * es % 16 == 0 && ldh * es % 16 == 0 && (!dres || lddr * es % 16 == 0);
+                         pitch_ok(rows, lddy * es) && pitch_ok(rows, ldh * es) && (!dres || pitch_ok(rows, lddr * es));
         e = dtype == QUEST_F32 ? launch_bwd_type<true>(a, vec, parts, st) : launch_bwd_type<false>(a, vec, parts, st);
         if (e != cudaSuccess) return cuda_fail(e);
     }
