@@ -16,7 +16,8 @@
 // copies, last products, sums of the parts, stores), with DRAM at 7 % (24 x 5504 x 2048).  Above that an SM takes in 54 bytes of
 // operands a cycle (0.17 us a stage of 17 KB with all products left out), spread nibbles counted as bytes: that is why 8-bit x, which
 // needs w spread, takes longer than 4-bit x.  Of a launch after the quantizer of x, fetching the first five k-blocks into L2 ahead saves
-// 0.3 us; sixteen cost the largest 10 %.
+// 0.3 us; sixteen cost the largest 10 %.  Tried: sums of the parts written to their owners (24 x 5504 x 2048 in thirds 7.1 us with remote
+// stores, 7.8 with bulk copies, 5.9 with remote reads); pairs of CTAs on 256 rows of w, unsplit (6.3); w fetched ahead by rows (no gain).
 #include <algorithm>
 
 #include "quest_mx_tcgen05.cuh"
