@@ -4,8 +4,11 @@
 // mma.sync m16n8k16 with the rows of w as the 16-wide side: 128 rows of w a CTA, as the tcgen05 products take, would leave most SMs
 // without one or cost sums over a cluster.  Codes become binary16 operands with the hardware conversions, two elements an
 // instruction and exactly (E2M1 has 2 and E4M3 4 significant bits); their scales, which may pass binary16's range, stay out:
-// a block of 32 is two products from zero, and its sums join the accumulators times 2^(sw + sx) in binary32:
-//     acc[n][m] += (2^sw[n] 2^sx[m]) sum_32 qw[n] qx[m]
+// a block of 32 is two products from zero, and its sums join the accumulators times one scale after the other in binary32:
+//     acc[n][m] += 2^sw[n] (2^sx[m] sum_32 qw[n] qx[m])
+// (the two scales alone may meet past 2^128 over sums that are 0, or less than 1).  A block's sum c is 0 or 2^-10 to 2^17 in steps
+// of 2^-10, so times a scale below 2^111 it neither overflows nor loses a bit (steps of 2^-137 at least), and the rest is one
+// rounding.  Warps that meet a scale of x of 2^65 or more take their sums once more, with the smaller scale of each pair first.
 //
 // A CTA takes 16 RT rows of w, its warps split K in groups of 128 elements.  w goes through shared memory (16-byte asynchronous
 // copies, two groups a warp in flight, rows 80 bytes apart so that reads meet no bank twice), because the four lanes that share a row
@@ -120,8 +123,62 @@ __device__ __forceinline__ uint32_t quantize_quarter(float *v, bool rotate, int 
     return s;
 }
 
+// The sums of a warp whatever the scales, into its place of the partial sums: 16 rows of w, eight of x and one block at a time, codes
+// straight from memory.  The smaller of two scales cannot make a block's sum overflow unless the whole does; a NaN counts as the smaller.
 template <int XB, int TT, int RT, bool FUSED>
-__global__ void __launch_bounds__(32 * WARPS)
+__device__ __forceinline__ void sums_of_any_scales(const FewArgs &a, const uint8_t *x_operands, const uint8_t *x_scales, float *mine) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int blocks = a.K / MX_BLOCK;
+#pragma unroll 1
+    for (int i = 0; i < RT * TT; ++i) {
+        const int n = blockIdx.x * (16 * RT) + 16 * (i / TT) + g, m0 = 8 * (i % TT);
+        float acc[4] = {};
+#pragma unroll 1
+        for (int block = 4 * warp; block < blocks; block = (block & 3) == 3 ? block + 4 * WARPS - 3 : block + 1) {
+            uint32_t w[2][4], x[4];
+            float sw[2], sx[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bool in = n + 8 * h < a.N;
+                const long long row = (long long)(n + 8 * h) * a.K;
+                f16_of_e2m1x8(in ? __ldg(reinterpret_cast<const uint32_t *>(a.wq + (row + block * MX_BLOCK + 8 * t) / 2)) : 0u, w[h]);
+                sw[h] = in ? mx_scale_f32(__ldg(a.sw + mx_scale_at(n + 8 * h, block, a.tiles))) : 0.0f;
+                const int m = m0 + 2 * t + h;
+                if constexpr (FUSED) sx[h] = m < a.M ? mx_scale_f32(x_scales[4 * (m * a.tiles) + block]) : 0.0f;
+                else sx[h] = m < a.M ? mx_scale_f32(__ldg(a.sx + mx_scale_at(m, block, a.tiles))) : 0.0f;
+            }
+            const bool in = m0 + g < a.M;
+            const long long at = (long long)(m0 + g) * a.K + block * MX_BLOCK + 8 * t;
+            if constexpr (FUSED) {
+                const uint4 q = in ? *reinterpret_cast<const uint4 *>(x_operands + g * x_pitch(a.tiles) + 64 * block + 16 * t) : make_uint4(0u, 0u, 0u, 0u);
+                x[0] = q.x; x[1] = q.y; x[2] = q.z; x[3] = q.w;
+            } else if constexpr (XB == 4) {
+                f16_of_e2m1x8(in ? __ldg(reinterpret_cast<const uint32_t *>(a.xq + at / 2)) : 0u, x);
+            } else {
+                const uint2 q = in ? __ldg(reinterpret_cast<const uint2 *>(a.xq + at)) : make_uint2(0u, 0u);
+                f16_of_e4m3x4(q.x, x);
+                f16_of_e4m3x4(q.y, x + 2);
+            }
+            const uint32_t a0[4] = {w[0][0], w[1][0], w[0][1], w[1][1]}, a1[4] = {w[0][2], w[1][2], w[0][3], w[1][3]};
+            float c[4];
+            mma_f16_first(c, a0, x);
+            mma_f16(c, a1, x + 2);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float least;
+                asm("min.NaN.f32 %0, %1, %2;" : "=f"(least) : "f"(sx[k & 1]), "f"(sw[k >> 1]));
+                acc[k] = __fmaf_rn(__fmul_rn(c[k], least), fmaxf(sx[k & 1], sw[k >> 1]), acc[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mine[(m0 + 2 * t + (k & 1)) * part_pitch(RT) + 16 * (i / TT) + 8 * (k >> 1) + g] = acc[k];
+    }
+}
+
+// Two CTAs to an SM where a round of them has that many (launch_mx_few_rows); elsewhere registers for one (16 x 2048 x 2048, 4 bits: 3.0 us
+// with 102 of them, 4.6 with 64).
+template <int XB, int TT, int RT, bool FUSED>
+__global__ void __launch_bounds__(32 * WARPS, TT == 1 && RT == 1 ? 2 : 1)
 mx_few_rows_kernel(const __grid_constant__ FewArgs a) {
     static_assert(!FUSED || TT == 1, "x is quantized on the way for up to eight rows");
     extern __shared__ __align__(16) uint8_t smem[];
@@ -190,6 +247,7 @@ mx_few_rows_kernel(const __grid_constant__ FewArgs a) {
         }
         __syncthreads();
     }
+    uint32_t large = 0;                          // bit 7 of a byte: a scale of x of 2^65 or more (or NaN)
     int slot = 0;
     for (int group = warp; group < a.tiles; group += WARPS, slot ^= 1) {
         const bool more = group + WARPS < a.tiles;
@@ -232,6 +290,8 @@ mx_few_rows_kernel(const __grid_constant__ FewArgs a) {
                 }
             }
         }
+#pragma unroll
+        for (int tt = 0; tt < TT; ++tt) large |= (xs[tt][0] & (xs[tt][0] << 1)) | (xs[tt][1] & (xs[tt][1] << 1));
         if (more) asm volatile("cp.async.wait_group 1;" ::: "memory");
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncwarp();
@@ -267,8 +327,8 @@ mx_few_rows_kernel(const __grid_constant__ FewArgs a) {
                     mma_f16_first(c, a0, xb[tt]);
                     mma_f16(c, a1, xb[tt] + 2);
                     float2 *p = reinterpret_cast<float2 *>(acc[r][tt]);
-                    p[0] = __ffma2_rn(make_float2(c[0], c[1]), __fmul2_rn(sx2[tt], make_float2(s0, s0)), p[0]);
-                    p[1] = __ffma2_rn(make_float2(c[2], c[3]), __fmul2_rn(sx2[tt], make_float2(s1, s1)), p[1]);
+                    p[0] = __ffma2_rn(__fmul2_rn(make_float2(c[0], c[1]), sx2[tt]), make_float2(s0, s0), p[0]);
+                    p[1] = __ffma2_rn(__fmul2_rn(make_float2(c[2], c[3]), sx2[tt]), make_float2(s1, s1), p[1]);
                 }
             }
         }
@@ -277,13 +337,17 @@ mx_few_rows_kernel(const __grid_constant__ FewArgs a) {
     __syncthreads();                             // every warp has left the ring
     float *part = reinterpret_cast<float *>(smem);               // [warp][token][row of w]
     constexpr int ROWS = RT * 16, TOKENS = TT * 8, P = part_pitch(RT);
+    if (__any_sync(0xffffffffu, (large & 0x80808080u) != 0)) {
+        sums_of_any_scales<XB, TT, RT, FUSED>(a, x_operands, x_scales, part + warp * TOKENS * P);     // (x lies behind the ring)
+    } else {
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int tt = 0; tt < TT; ++tt)
+            for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-                part[(warp * TOKENS + 8 * tt + 2 * t + (c & 1)) * P + 16 * r + 8 * (c >> 1) + g] = acc[r][tt][c];
+                for (int c = 0; c < 4; ++c)
+                    part[(warp * TOKENS + 8 * tt + 2 * t + (c & 1)) * P + 16 * r + 8 * (c >> 1) + g] = acc[r][tt][c];
+    }
     __syncthreads();
     const int live = min(WARPS, a.tiles);
     for (int i = threadIdx.x; i < TOKENS * ROWS; i += 32 * WARPS) {
