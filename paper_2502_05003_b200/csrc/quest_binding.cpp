@@ -653,14 +653,25 @@ PyObject *linear_bwd_mx(PyObject *const *a) {
     const bool want_x = bool_arg(a[8]) || a[6] != Py_None, want_w = bool_arg(a[9]) || a[7] != Py_None;
     const int64_t bytes = (int64_t)quest_bwd_mx_workspace_bytes(M, N, K);
     if ((!want_x && !want_w) || !bytes) throw NotPlain();
-    auto saved = [&](PyObject *key, bool used, int64_t n) -> const uint8_t * {
-        if (!used) return nullptr;
-        PyObject *v = item(a[1], key);
-        if (!v) throw NotPlain();
-        return (const uint8_t *)room_beside(v, dy, at::kByte, n);
+    auto saved = [&](PyObject *key, bool used) {
+        PyObject *v = used ? item(a[1], key) : nullptr;
+        if (used && !v) throw NotPlain();
+        return v;
     };
-    const uint8_t *xq = saved(k_xq, want_w, M * K * bits / 8), *sx = saved(k_sx, want_w, mx_scales(M, K));
-    const uint8_t *wq = saved(k_wq, want_x, N * K / 2), *sw = saved(k_sw, want_x, mx_scales(N, K));
+    // codes have the shape that bits and K say: those of another layer, width or batch would be read as if they did
+    auto codes = [&](PyObject *key, bool used, int64_t rows, int width) -> const uint8_t * {
+        PyObject *v = saved(key, used);
+        if (!v) return nullptr;
+        const at::Tensor &t = rows_beside(v, dy);
+        if (t.scalar_type() != at::kByte || !t.is_contiguous() || t.size(0) != rows || t.size(1) * 8 != K * width) throw NotPlain();
+        return (const uint8_t *)t.data_ptr();
+    };
+    auto scales = [&](PyObject *key, bool used, int64_t rows) -> const uint8_t * {
+        PyObject *v = saved(key, used);
+        return v ? (const uint8_t *)room_beside(v, dy, at::kByte, mx_scales(rows, K)) : nullptr;
+    };
+    const uint8_t *xq = codes(k_xq, want_w, M, bits), *sx = scales(k_sx, want_w, M);
+    const uint8_t *wq = codes(k_wq, want_x, N, 4), *sw = scales(k_sw, want_x, N);
     c10::cuda::CUDAGuard guard(dy.device());
     for (PyObject *o : {a[6], a[7]})
         if (o != Py_None) ot = beside(o, dy).scalar_type();
