@@ -548,6 +548,14 @@ def _kept(name: str, out: dict, key: str, shape, dtype, device):
     return t
 
 
+def _workspace_bytes_of(name: str, t) -> int:
+    if t is None:
+        return 0
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: workspace must be contiguous")
+    return t.numel() * t.element_size()
+
+
 def _mx_codes_of(name: str, key: str, t: torch.Tensor, cols: int, bits: int):
     if t.dtype != torch.uint8 or t.dim() != 2 or not t.is_contiguous() or t.shape[1] * 8 != cols * bits:
         raise ValueError(f"{name}: {key} must be a contiguous uint8 tensor [rows, {cols * bits // 8}]")
@@ -729,7 +737,7 @@ def quest_linear_bwd_mx(dy: torch.Tensor, fwd: dict, bits_x: int, had_block: int
         _lib.check(_lib.load().quest_linear_bwd_mx(
             _p(dy), M, N, K, bits_x, had_block, *[_p(fwd[k]) if k in used else None for k in ("xq", "sx", "wq", "sw")],
             _p(out["dx"]), _p(out["dw"]), _dtype_code(some) if some is not None else F32, _p(workspace),
-            workspace.numel() * workspace.element_size(), _stream()))
+            _workspace_bytes_of(name, workspace), _stream()))
     return out
 
 
@@ -815,6 +823,5 @@ def quest_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, r
             workspace = torch.empty(quest_rmsnorm_bwd_workspace_bytes(rows, cols), dtype=torch.uint8, device=dy.device)
         _lib.check(_lib.load().quest_rmsnorm_bwd(
             _p(dy), _p(h), _p(dres), _dtype_code(dy), lddy, ldh, lddr, _p(weight), _dtype_code(weight), _p(rstd), rows, cols,
-            _p(out["dx"]), _p(out["dw"]), _p(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0,
-            _stream()))
+            _p(out["dx"]), _p(out["dw"]), _p(workspace), _workspace_bytes_of(name, workspace), _stream()))
     return out
