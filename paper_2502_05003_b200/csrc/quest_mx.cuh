@@ -97,11 +97,6 @@ __device__ __forceinline__ float mx_inverse_scale(uint32_t s) { return s == 255u
 __device__ __forceinline__ float mx_scale_f32(uint32_t s) {
     return __uint_as_float(s == 255u ? 0x7FC00000u : s == 0u ? 0x00400000u : s << 23);
 }
-// The same in bfloat16, twice in a word.
-__device__ __forceinline__ uint32_t mx_scale_bf16x2(uint32_t s) {
-    const uint32_t h = s == 255u ? 0x7FC0u : s == 0u ? 0x0040u : s << 7;
-    return h * 0x10001u;
-}
 
 // Eight elements -> a word of E2M1 codes; four elements -> a word of E4M3 bytes.  To nearest, ties to even, saturating.
 __device__ __forceinline__ uint32_t mx_e2m1x8(const float *t) {

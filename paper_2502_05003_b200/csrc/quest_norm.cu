@@ -466,9 +466,12 @@ cudaError_t launch_bwd_type(const NormBwdArgs &a, bool vec, int &parts, cudaStre
         // short rows, many of them: a warp each (16384 x 512 bfloat16 16 us, a CTA each 22)
         if (chunks <= 64 && a.rows >= 1024)
             return chunks <= 32 ? launch_bwd<F32, true, 1, 128, 4, true, true>(a, parts, st) : launch_bwd<F32, true, 2, 128, 4, true, true>(a, parts, st);
+        if constexpr (F32) {                     // rows of up to 16384 columns: bfloat16 has at most 2048 chunks
+            if (chunks > 2048) return launch_bwd<F32, true, 8, 512, 1, false>(a, parts, st);
+        }
         return chunks <= 256 ? launch_bwd<F32, true, 2, 128, 4, true>(a, parts, st) : chunks <= 512 ? launch_bwd<F32, true, 2, 256, 2, true>(a, parts, st)
              : chunks <= 1024 ? launch_bwd<F32, true, 2, 512, 1, true>(a, parts, st) : chunks <= 1536 ? launch_bwd<F32, true, 3, 512, 1, true>(a, parts, st)
-             : chunks <= 2048 ? launch_bwd<F32, true, 4, 512, 1, false>(a, parts, st) : launch_bwd<F32, true, 8, 512, 1, false>(a, parts, st);
+             : launch_bwd<F32, true, 4, 512, 1, false>(a, parts, st);
     }
     return a.cols <= 1024 ? launch_bwd<F32, false, 4, 256, 2, true>(a, parts, st) : a.cols <= 4096 ? launch_bwd<F32, false, 4, 1024, 1, true>(a, parts, st)
          : a.cols <= 8192 ? launch_bwd<F32, false, 8, 1024, 1, false>(a, parts, st) : launch_bwd<F32, false, 16, 1024, 1, false>(a, parts, st);
@@ -499,8 +502,10 @@ cudaError_t launch_fwd(const NormArgs &a, bool vec, cudaStream_t st) {
         return chunks <= 32 ? launch_row_warp<F32, true, 1, MX>(a, rows, st) : chunks <= 64 ? launch_row_warp<F32, true, 2, MX>(a, rows, st)
                                                                                             : launch_row_warp<F32, true, 4, MX>(a, rows, st);
     if (chunks <= 256 && a.rows <= 2 * num_sms()) return launch_row_cta<F32, true, 1, MX>(a, rows, chunks, st);
-    return chunks <= 512 ? launch_row_cta<F32, true, 2, MX>(a, rows, chunks, st) : chunks <= 2048 ? launch_row_cta<F32, true, 4, MX>(a, rows, chunks, st)
-                                                                                                  : launch_row_cta<F32, true, 8, MX>(a, rows, chunks, st);
+    if constexpr (F32) {                         // (bfloat16: at most 2048 chunks)
+        if (chunks > 2048) return launch_row_cta<F32, true, 8, MX>(a, rows, chunks, st);
+    }
+    return chunks <= 512 ? launch_row_cta<F32, true, 2, MX>(a, rows, chunks, st) : launch_row_cta<F32, true, 4, MX>(a, rows, chunks, st);
 }
 
 }  // namespace
