@@ -357,14 +357,16 @@ int quest_dequantize_mx(const uint8_t *codes, const uint8_t *scales, int64_t row
  *   y                device out [M x N], y_dtype, row stride ldy_elems
  *
  * quest_linear_fwd_mx -- the layer: x (and w unless w_is_cached is 1) quantized as quest_quantize_mx does, then the product.
- *   xq, sx           device out: codes and scales of x, for a backward pass; both may be NULL where M <= 8, M K <= 4096
- *                    and N <= 7104: x is then quantized inside the product and nothing but y is written
+ *   xq, sx           device out: codes and scales of x, for a backward pass; both may be NULL where
+ *                    quest_mx_codes_optional(M, N, K) is 1 (M <= 8, M K <= 4096 and N <= 7104; else it is 0): x is then
+ *                    quantized inside the product and nothing but y is written
  *   wq, sw           device out, or inputs with w_is_cached = 1 (w may be NULL then)
  * The order of the sums over K depends on M, N, K and bits_x; equal calls give equal bits.
  * No workspace.  Errors as for quest_linear_fwd.  M = 0 or N = 0: the operand that is not empty is quantized, nothing else is done.
  */
 int quest_gemm_mx(const uint8_t *xq, const uint8_t *sx, int bits_x, const uint8_t *wq, const uint8_t *sw,
                   int64_t M, int64_t N, int64_t K, void *y, int y_dtype, int64_t ldy_elems, void *stream);
+int quest_mx_codes_optional(int64_t M, int64_t N, int64_t K);
 int quest_linear_fwd_mx(const void *x, int x_dtype, int64_t ldx, const void *w, int w_dtype, int64_t ldw,
                         int64_t M, int64_t N, int64_t K, int bits_x, int had_block, void *y, int y_dtype, int64_t ldy_elems,
                         uint8_t *xq, uint8_t *sx, uint8_t *wq, uint8_t *sw, int w_is_cached, void *stream);

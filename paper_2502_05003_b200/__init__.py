@@ -634,13 +634,18 @@ def quest_gemm_mx(xq: torch.Tensor, sx: torch.Tensor, bits_x: int, wq: torch.Ten
     return y
 
 
+def quest_mx_codes_optional(M: int, N: int, K: int) -> bool:
+    """Whether ``quest_linear_fwd_mx`` can quantize x inside the product: M up to 8, M K up to 4096, N up to 7104."""
+    return bool(_lib.load().quest_mx_codes_optional(M, N, K))
+
+
 def quest_linear_fwd_mx(x: torch.Tensor, w: torch.Tensor, bits_x: int = 8, had_block: int = 1, out_dtype=None,
                         y: torch.Tensor = None, saved: dict = None, w_cached: dict = None, want_codes: bool = True) -> dict:
     """The microscaled layer, y = x w^T with x in ``bits_x`` bits and w in 4: returns {"y", "xq", "sx", "wq", "sw"}.
 
     ``saved`` may carry preallocated tensors for the codes and scales; ``w_cached`` = {"wq", "sw"} holds weights that are quantized
-    already (then ``w`` may be None).  With ``want_codes`` false up to 8 rows of x (M K up to 4096, N up to 7104) are quantized inside the
-    product and their codes are not stored (None); more rows need the room all the same.  ``x`` or ``w`` whose rows do not start on
+    already (then ``w`` may be None).  With ``want_codes`` false up to 8 rows of x (where ``quest_mx_codes_optional(M, N, K)``) are quantized
+    inside the product and their codes are not stored (None); more rows need the room all the same.  ``x`` or ``w`` whose rows do not start on
     16-byte boundaries, or with another inner stride, is copied first."""
     done = _lib.binding().linear_fwd_mx(x, w, bits_x, had_block, out_dtype, y, saved, w_cached, want_codes)
     if done is not None:
@@ -677,7 +682,7 @@ def quest_linear_fwd_mx(x: torch.Tensor, w: torch.Tensor, bits_x: int = 8, had_b
             _mx_scales_of(name, "sw", out["sw"], N, K)
         _kept(name, out, "wq", (N, K // 2), torch.uint8, dev)
         _kept(name, out, "sw", (quest_mx_scales_bytes(N, K),), torch.uint8, dev)
-        if want_codes or M > 8 or M * K > 4096 or N > 7104:
+        if want_codes or not quest_mx_codes_optional(M, N, K):
             _kept(name, out, "xq", (M, K * bits_x // 8), torch.uint8, dev)
             _kept(name, out, "sx", (quest_mx_scales_bytes(M, K),), torch.uint8, dev)
         else:

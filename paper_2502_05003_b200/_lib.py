@@ -18,7 +18,7 @@ EXPORTS = (
     "quest_linear_fwd_weight_only", "quest_weight_only_workspace_bytes",
     "quest_mlp_fwd", "quest_mlp_workspace_bytes", "quest_linear_fwd_quantize", "quest_linear_fwd_contract",
     "quest_selftest_bounded_wait",
-    "quest_mx_scales_bytes", "quest_quantize_mx", "quest_dequantize_mx", "quest_gemm_mx", "quest_linear_fwd_mx",
+    "quest_mx_scales_bytes", "quest_quantize_mx", "quest_dequantize_mx", "quest_gemm_mx", "quest_mx_codes_optional", "quest_linear_fwd_mx",
     "quest_linear_bwd_mx", "quest_bwd_mx_workspace_bytes",
     "quest_rmsnorm_fwd", "quest_rmsnorm_bwd", "quest_rmsnorm_bwd_workspace_bytes",
 )
@@ -89,6 +89,8 @@ def load() -> ctypes.CDLL:
     L.quest_dequantize_mx.argtypes = [vp, vp, i64, i64, ci, vp, ci, vp]
     L.quest_gemm_mx.restype = ci
     L.quest_gemm_mx.argtypes = [vp, vp, ci, vp, vp, i64, i64, i64, vp, ci, i64, vp]
+    L.quest_mx_codes_optional.restype = ci
+    L.quest_mx_codes_optional.argtypes = [i64, i64, i64]
     L.quest_linear_fwd_mx.restype = ci
     L.quest_linear_fwd_mx.argtypes = [vp, ci, i64, vp, ci, i64, i64, i64, i64, ci, ci, vp, ci, i64, vp, vp, vp, vp, ci, vp]
     L.quest_linear_bwd_mx.restype = ci

@@ -619,7 +619,7 @@ PyObject *linear_fwd_mx(PyObject *const *a) {
     if (N < 1) throw NotPlain();
     uint8_t *wq = (uint8_t *)keep(out, k_wq, x, {N, K / 2}, at::kByte), *sw = (uint8_t *)keep(out, k_sw, x, {mx_scales(N, K)}, at::kByte);
     uint8_t *xq = nullptr, *sx = nullptr;
-    if (codes || M > 8 || M * K > 4096 || N > 7104) {
+    if (codes || !quest_mx_codes_optional(M, N, K)) {
         xq = (uint8_t *)keep(out, k_xq, x, {M, K * bits / 8}, at::kByte);
         sx = (uint8_t *)keep(out, k_sx, x, {mx_scales(M, K)}, at::kByte);
     } else {

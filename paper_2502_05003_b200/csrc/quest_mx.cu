@@ -250,6 +250,10 @@ int quest_gemm_mx(const uint8_t *xq, const uint8_t *sx, int bits_x, const uint8_
     return s;
 }
 
+int quest_mx_codes_optional(int64_t M, int64_t N, int64_t K) {
+    return mx_rows_ok(M) && mx_rows_ok(N) && mx_cols_ok(K) && mx_fuses_quantizer(M, N, K);
+}
+
 int quest_linear_fwd_mx(const void *x, int x_dtype, int64_t ldx, const void *w, int w_dtype, int64_t ldw, int64_t M, int64_t N,
                         int64_t K, int bits_x, int had_block, void *y, int y_dtype, int64_t ldy_elems, uint8_t *xq, uint8_t *sx,
                         uint8_t *wq, uint8_t *sw, int w_is_cached, void *stream) {
