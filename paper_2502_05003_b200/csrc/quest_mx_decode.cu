@@ -8,7 +8,7 @@
 //     acc[n][m] += 2^sw[n] (2^sx[m] sum_32 qw[n] qx[m])
 // (the two scales alone may meet past 2^128 over sums that are 0, or less than 1).  A block's sum c is 0 or 2^-10 to 2^17 in steps
 // of 2^-10, so times a scale below 2^111 it neither overflows nor loses a bit (steps of 2^-137 at least), and the rest is one
-// rounding.  Warps that meet a scale of x of 2^65 or more take their sums once more, with the smaller scale of each pair first.
+// rounding.  Warps (FUSED: CTAs) that meet a scale of x of 2^65 or more take their sums once more, the smaller scale of each pair first.
 //
 // A CTA takes 16 RT rows of w, its warps split K in groups of 128 elements.  w goes through shared memory (16-byte asynchronous
 // copies, two groups a warp in flight, rows 80 bytes apart so that reads meet no bank twice), because the four lanes that share a row
@@ -125,8 +125,9 @@ __device__ __forceinline__ uint32_t quantize_quarter(float *v, bool rotate, int 
 
 // The sums of a warp whatever the scales, into its place of the partial sums: 16 rows of w, eight of x and one block at a time, codes
 // straight from memory.  The smaller of two scales cannot make a block's sum overflow unless the whole does; a NaN counts as the smaller.
+// Not inlined: in between the kernel's own instructions it costs a lone call of 1 x 2048 x 2048 0.15 us.
 template <int XB, int TT, int RT, bool FUSED>
-__device__ __forceinline__ void sums_of_any_scales(const FewArgs &a, const uint8_t *x_operands, const uint8_t *x_scales, float *mine) {
+__device__ __noinline__ void sums_of_any_scales(const FewArgs &a, const uint8_t *x_operands, const uint8_t *x_scales, float *mine) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int blocks = a.K / MX_BLOCK;
 #pragma unroll 1
@@ -213,6 +214,7 @@ mx_few_rows_kernel(const __grid_constant__ FewArgs a) {
     if (warp < a.tiles) request(warp, 0);
     // FUSED: operands of x, rows of whole groups, and behind them four scale bytes a group
     uint8_t *x_operands = smem + WARPS * 2 * GROUP_BYTES, *x_scales = x_operands + a.M * x_pitch(a.tiles);
+    int any_large = 0;                           // a scale of x of 2^65 or more (or NaN)
     if constexpr (FUSED) {
         const int quarters = 16 * a.tiles;       // of a row
         for (int i = threadIdx.x; i < (a.M * quarters + 31) / 32 * 32; i += 32 * WARPS) {
@@ -242,12 +244,13 @@ mx_few_rows_kernel(const __grid_constant__ FewArgs a) {
             const uint32_t s = quantize_quarter<XB>(v, a.rotate, lane, h);      // a block's four quarters are lanes of one warp
             if (m < a.M) {
                 *reinterpret_cast<uint4 *>(x_operands + m * x_pitch(a.tiles) + 16 * q) = make_uint4(h[0], h[1], h[2], h[3]);
+                any_large |= s >= 192u;
                 if ((q & 3) == 0) x_scales[4 * (m * a.tiles) + (q >> 2)] = (uint8_t)s;
             }
         }
-        __syncthreads();
+        any_large = __syncthreads_or(any_large);
     }
-    uint32_t large = 0;                          // bit 7 of a byte: a scale of x of 2^65 or more (or NaN)
+    uint32_t large = 0;                          // bit 7 of a byte: the same in the codes' scales
     int slot = 0;
     for (int group = warp; group < a.tiles; group += WARPS, slot ^= 1) {
         const bool more = group + WARPS < a.tiles;
@@ -290,8 +293,9 @@ mx_few_rows_kernel(const __grid_constant__ FewArgs a) {
                 }
             }
         }
+        if constexpr (!FUSED)
 #pragma unroll
-        for (int tt = 0; tt < TT; ++tt) large |= (xs[tt][0] & (xs[tt][0] << 1)) | (xs[tt][1] & (xs[tt][1] << 1));
+            for (int tt = 0; tt < TT; ++tt) large |= (xs[tt][0] & (xs[tt][0] << 1)) | (xs[tt][1] & (xs[tt][1] << 1));
         if (more) asm volatile("cp.async.wait_group 1;" ::: "memory");
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncwarp();
@@ -337,7 +341,8 @@ mx_few_rows_kernel(const __grid_constant__ FewArgs a) {
     __syncthreads();                             // every warp has left the ring
     float *part = reinterpret_cast<float *>(smem);               // [warp][token][row of w]
     constexpr int ROWS = RT * 16, TOKENS = TT * 8, P = part_pitch(RT);
-    if (__any_sync(0xffffffffu, (large & 0x80808080u) != 0)) {
+    if constexpr (!FUSED) any_large = __any_sync(0xffffffffu, (large & 0x80808080u) != 0);
+    if (any_large) {
         sums_of_any_scales<XB, TT, RT, FUSED>(a, x_operands, x_scales, part + warp * TOKENS * P);     // (x lies behind the ring)
     } else {
 #pragma unroll
