@@ -50,9 +50,9 @@ int launch_mx_few_rows(const void *x, int x_dtype, int64_t ldx, const uint8_t *x
                        cudaStream_t st);
 
 // Which of the three.  Up to 32 rows go without tensor memory while w is small: its rows fill one round of CTAs, and K is short enough
-// for one CTA to walk.  Time of the exchanged tiles over that kernel's, 8 and 4 bits: 8 x 2048 x 2048 1.12 / 1.02, x 4096 0.91 / 0.79,
-// x 8192 0.75 / 0.62; 8 x 4096 x 2048 1.17 / 1.06, 8 x 8192 x 2048 0.75 / 0.62; 16 x 2048 x 2048 1.15 / 0.83, x 2560 0.98 / 0.72; 24 x 2048 x
-// 1024 0.96 / 1.11, x 1536 0.92 / 1.08, x 2048 0.95 / 0.96; 32 x 2048 x 768 0.92 / 0.96; 32 x 32000 x 4096 0.21 / 0.25.
+// for one CTA to walk.  Time of the exchanged tiles over that kernel's, 8 and 4 bits: 8 x 2048 x 2048 1.13 / 0.96, x 4096 0.90 / 0.73,
+// x 8192 0.70 / 0.55; 8 x 4096 x 2048 1.41 / 1.18, 8 x 8192 x 2048 0.73 / 0.54; 16 x 2048 x 2048 1.13 / 1.09, x 2560 1.01 / 0.89; 24 x 2048 x
+// 1024 1.06 / 1.14, x 1536 0.96 / 1.01, x 2048 1.02 / 0.95; 32 x 2048 x 768 0.93 / 0.83; 32 x 32000 x 4096 0.22 / 0.20.
 // Above, the exchanged tiles against pairs of CTAs on 256 rows of x: 64 x 4096 x 4096 0.71 / 0.87, 128 x 2048 x 8192 0.52 / 0.67;
 // more than 128 rows 0.5 .. 1.04 where w fills a side of 128 and the tiles take half of the SMs (K is split) or one
 // short round, else 0.8 .. 1.3.
@@ -65,7 +65,7 @@ inline MxProduct mx_product(int64_t M, int64_t N, int64_t K, int bits_x) {
     const bool fits = N >= 128 && (2 * tiles <= MX_SMS || (tiles <= MX_SMS && K <= (bits_x == 4 ? 2048 : 1024)));
     return M <= 128 || fits ? MxProduct::thin : MxProduct::wide;
 }
-// Whether the product of few rows quantizes x itself: up to eight of which a thread of the CTA takes one quarter of a block.  More, and
+// Whether the product of few rows quantizes x itself (quest_mx_codes_optional): up to eight of which a thread of the CTA takes one quarter of a block.  More, and
 // a launch of the quantizer in front costs less (8 x 2048 x 2048: 7.7 us against 4.9; 1 x 2048 x 2048: 3.8 against 4.2, 2 x 2048 x 2048 4.2 against 4.3).
 inline bool mx_fuses_quantizer(int64_t M, int64_t N, int64_t K) { return M <= 8 && M * K <= 4096 && N <= 48 * MX_SMS; }
 

@@ -17,10 +17,10 @@
 // FUSED (mx_fuses_quantizer): every CTA quantizes x while the first copies of w are under way, four
 // threads to a block, and leaves operands and scale bytes in shared memory.  One launch, and the host pays for one.
 //
-// Device time back to back, weights out of L2: 1 x 2048 x 2048 3.8 us fused, 3.0 from codes (the floor of 2.3 MB is 0.35: launch,
-// one round trip to memory, conversions and sums); 16 x 2048 x 2048 3.7 from codes, where conversions, products and scaling fill 29 % of
-// the issue slots.  (bfloat16 operands unpacked with shifts and masks, every CTA quantizing all of x: 7.4 us for 24 x 5504 x 2048 from
-// codes, 17.2 from values, against 7.1 for this form.)
+// Device time back to back, weights out of L2: 1 x 2048 x 2048 3.7 us fused, 2.9 from codes (the floor of 2.3 MB is 0.35: launch,
+// one round trip to memory, conversions and sums); 16 x 2048 x 2048 3.3 from codes, where conversions, products and scaling fill 30 % of
+// the issue slots.  (bfloat16 operands unpacked with shifts and masks took 1.04 times the time of the conversions, and every CTA
+// quantizing all of 24 rows of x 2.4 times, on 24 x 5504 x 2048, which the exchanged tiles take now.)
 #include <algorithm>
 
 #include "quest_mx.cuh"
@@ -30,9 +30,9 @@ namespace {
 
 constexpr int WARPS = 16;
 constexpr int PITCH = 80;                        // bytes between the rows of a group (64 bytes of codes)
-// FUSED: bytes between the rows of x as operands; eight lanes read 64 bytes each of two rows without a conflict
 // floats between the tokens of a warp's partial sums: the 32 lanes of a store meet 32 banks
 __host__ __device__ constexpr int part_pitch(int rt) { return 16 * rt + 4; }
+// FUSED: bytes between the rows of x as operands; eight lanes read 64 bytes each of two rows without a conflict
 __host__ __device__ constexpr int x_pitch(int tiles) { return 256 * tiles + 64; }
 
 struct FewArgs {
@@ -394,8 +394,9 @@ int launch_mx_few_rows(const void *x, int x_dtype, int64_t ldx, const uint8_t *x
                        cudaStream_t st) {
     const FewArgs a = {x, xq, sx, (long long)ldx, wq, sw, (int)M, (int)N, (int)K, (int)((K + 127) / 128), y, (long long)ldy,
                        x_dtype == QUEST_F32, had_block == 32, y_dtype == QUEST_F32};
-    // rows of w a CTA: as few as one round of CTAs allows, for up to eight rows of x two 16-row CTAs to an SM (24 x 5504 x 2048 from
-    // codes: 48 rows a CTA 7.8 us, 32 10.4, 16 11.3; 8 x 4096 x 4096: 16 rows 5.6, 48 6.5).  Longer w does not come here (mx_product)
+    // rows of w a CTA: as few as one round of CTAs allows, for up to eight rows of x two 16-row CTAs to an SM.  From codes, us with 16 rows a
+    // CTA and with more: 1 x 4736 x 2048 3.3, 48 rows 3.9; 1 x 5504 x 2048 4.7, 3.9; 8 x 4096 x 4096 5.4, 6.1; 8 x 5504 x 4096 8.1, 6.2;
+    // 16 x 2368 x 2048 3.5, 32 rows 4.0; 16 x 2400 x 2048 5.6, 4.3; 24 x 2400 x 1280 5.8, 4.8.  Longer w does not come here (mx_product)
     const int64_t sms = num_sms();
     const int rt = M <= 8 ? (N <= 32 * sms ? 1 : 3) : N <= 16 * sms ? 1 : 2;
     const cudaError_t e = bits_x == 4 ? launch_tokens<4>(a, rt, st) : launch_tokens<8>(a, rt, st);

@@ -135,7 +135,8 @@ constexpr int row_threads(int vpt) { return vpt <= 1 ? 256 : vpt <= 4 || vpt == 
 
 // VPT chunks to a thread; a row belongs to a warp (ROW_WARP, four rows to a CTA) or to the CTA.  MX: 0, or the bits of the
 // output: the 32 / V neighbouring lanes that hold a block agree on its scale.  8192 x 2048 with residual: bfloat16 22.1 us (6.1
-// TB/s), 8-bit MX out 22.9, rotated 27 (there the ALU pipe is busy two thirds of the time); binary32 41.5 (6.5 TB/s).
+// TB/s), MX out in 8 or 4 bits 22.9, rotated 27 (there the ALU pipe is busy two thirds of the time); binary32 41.5 (6.5 TB/s), MX out 35, rotated
+// 39.  Rows that no 16-byte access divides, an element at a time: 8192 x 2047 52 in both types.
 template <bool F32, bool VEC, int VPT, bool ROW_WARP, int MX>
 __global__ void __launch_bounds__(ROW_WARP ? 128 : row_threads(VPT))
 rmsnorm_kernel(const __grid_constant__ NormArgs a) {
@@ -272,7 +273,7 @@ struct NormBwdArgs {
 // share of dw stays in registers over all of the rows.  AHEAD: the next row is requested before the present one is reduced,
 // which keeps loads in flight over the barrier.  Bound by memory; 8192 x 2048 bfloat16 with dres: 24.1 us and 3.1 for the sum of
 // dw's parts, 4.9 TB/s together (four rows to a barrier without AHEAD: 32 us; half or all of the chunks in a thread: 28 .. 33).
-// The weight stays in registers where the chunks are few.
+// The weight stays in registers where the chunks are few.  binary32 46; an element at a time, 8192 x 2047 87 (bfloat16) and 85.
 template <bool F32, bool VEC, int VPT, int THREADS, int CTAS, bool AHEAD, bool ROW_WARP>
 __global__ void __launch_bounds__(THREADS, CTAS)
 rmsnorm_bwd_kernel(const __grid_constant__ NormBwdArgs a) {
